@@ -585,6 +585,92 @@ int darts_debug_gumbel(const float* d_u, float* d_g, int64_t n, void* stream);
 int darts_debug_gumbel_fast(const float* d_u, float* d_g, int64_t n, void* stream);
 float darts_sampler_gumbel_bound(void);
 
+/* ------------------------------------------- routing, 8-bit integer layers */
+/* An expert layer served in 8 bits, and its projections: the router, rows of
+ * activations to 8-bit codes, the product of codes, and the experts'
+ * feed-forward.  Codes are signed bytes in [-127, 127]; a code times its row's
+ * scale (activations: one per token; weights: one per output channel) is the
+ * value it stands for.  Weights are the caller's: [N][K] codes and [N] float32
+ * scales.  Stateless, like the calls above; nothing is allocated, so every call
+ * may be captured into a graph.                                            */
+
+typedef enum { DARTS_SCORE_SOFTMAX = 0, DARTS_SCORE_SIGMOID = 1 } darts_score;
+
+/* Route rows to experts.  With l the row's logits and b the bias (NULL: 0):
+ *   s_e = softmax(l)_e or 1 / (1 + exp(-l_e)),   t_e = s_e + b_e
+ * An expert whose logit or bias is -inf cannot be chosen.  The experts form
+ * n_groups groups of n_experts / n_groups consecutive ids; a group's value is
+ * the sum of its group_best (1 or 2) largest t, the top_groups groups of the
+ * largest value stay (1 and 1: every expert), and of their experts the top_k
+ * largest t are chosen, in that order.  Ties go to the lower id or group.  The
+ * weight of a chosen expert is its s (without the bias), divided by the sum of
+ * the chosen ones' when renorm != 0 (0 if that sum is 0), times factor.
+ * Scores are 64-bit (float32 weights come out); two that agree to 42 bits count
+ * as equal.
+ *   d_logits  [n_rows] rows of n_experts (bf16 or f32), ld elements apart
+ *   d_bias    NULL or [n_experts] float32
+ *   d_ids     [n_rows][top_k] int32 out
+ *   d_weights [n_rows][top_k] float32 out
+ * Places for which no expert is left (a row masked out whole has none at all)
+ * get id -1 and weight 0.  A row with a NaN or +inf logit, and every row when
+ * the bias holds one, gets ids -1 and weights NaN.  Errors: DARTS_EINVAL unless
+ * 1 <= n_experts <= 1024, 1 <= top_k <= min(64, n_experts), ld >= n_experts,
+ * 1 <= n_groups <= 64 divides n_experts, 1 <= top_groups <= n_groups, group_best
+ * is 1 or 2, and factor is finite.                                         */
+int darts_moe_route(const void* d_logits, int64_t ld, int32_t n_rows, int32_t n_experts, int32_t dtype,
+                    int32_t score, const float* d_bias, int32_t n_groups, int32_t top_groups,
+                    int32_t group_best, int32_t top_k, int32_t renorm, float factor, int32_t* d_ids,
+                    float* d_weights, void* stream);
+
+/* Rows of activations to codes.  With a the largest magnitude of the row, in
+ * float32 arithmetic:
+ *   d_scale[r] = a / 127,   d_q[r][c] = rint(x[r][c] * (127 / a))   (half to even)
+ * A row with a < 2^-119 gets scale 0 and codes 0, a row with an infinity or NaN
+ * scale NaN and codes 0 (its products are NaN).
+ *   d_x     rows of cols elements (bf16 or f32), ldx elements apart
+ *   d_q     [rows][cols] int8 out,  d_scale [rows] float32 out
+ * DARTS_EINVAL for rows < 0, cols < 1 or ldx < cols.                       */
+int darts_quantize_rows(const void* d_x, int64_t ldx, int32_t rows, int32_t cols, int32_t dtype, int8_t* d_q,
+                        float* d_scale, void* stream);
+
+/* The decoder's dense projection on codes: with acc = A[M,K] . W[N,K]^T summed
+ * exactly in 32-bit integers,
+ *   C[m][n] = acc[m][n] * d_a_scale[m] * d_w_scale[n]   (float32)
+ * and the epilogues of darts_gemm: 0 float32 stored, 1 bf16 stored, 2 added to a
+ * float32 d_c, 3 SwiGLU (W rows and their scales interleaved in groups of 16;
+ * d_c [M][N/2] bf16).
+ *   d_a [M][K], d_w [N][K] codes, 16-byte aligned; K and N multiples of 16 (N of
+ *   32 for SwiGLU), K <= 131072 (so that the sum fits).  d_workspace must hold
+ *   darts_gemm_i8_workspace_bytes(M, N, K) bytes, 16-byte aligned.         */
+size_t darts_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K);
+int darts_gemm_i8(const int8_t* d_a, const float* d_a_scale, const int8_t* d_w, const float* d_w_scale,
+                  void* d_c, int32_t M, int32_t N, int32_t K, int32_t epilogue, void* d_workspace,
+                  size_t workspace_bytes, void* stream);
+
+/* Feed-forward of routed experts on codes.  Every (row, slot) pair with an id in
+ * [0, n_experts) goes through its expert:
+ *   h = bf16(silu(g) * u) with g, u the gate and up products of x's codes (as
+ *   darts_quantize_rows makes them), y = bf16(the down product of h's codes),
+ *   out[r] = sum_j weights[r][j] * y_j   (float32, slot order)
+ * Pairs with another id add nothing (and NaN where their weight is NaN).
+ *   d_x        [n_rows][d_model] bf16
+ *   d_ids, d_weights  [n_rows][top_k] int32 and float32, as darts_moe_route
+ *              writes them; an id may come twice in a row
+ *   d_w_gu     [n_experts][2*expert_ffn][d_model] codes, gate and up rows
+ *              interleaved in groups of 16; d_s_gu [n_experts][2*expert_ffn]
+ *   d_w_down   [n_experts][d_model][expert_ffn] codes; d_s_down [n_experts][d_model]
+ *   d_out      [n_rows][d_model]: epilogue 1 bf16 stored, 2 added to float32
+ *   d_workspace darts_moe_ffn_i8_workspace_bytes(...) bytes, 256-byte aligned
+ * Codes, d_x and d_out are 16-byte aligned.  d_model and expert_ffn are multiples of 16
+ * up to 131072, n_experts <= 1024, top_k <= 64, n_rows * top_k <= 4194240.
+ * Calls that overlap in time need workspaces of their own, captured graphs too. */
+size_t darts_moe_ffn_i8_workspace_bytes(int32_t n_rows, int32_t d_model, int32_t n_experts, int32_t top_k,
+                                        int32_t expert_ffn);
+int darts_moe_ffn_i8(const void* d_x, const int32_t* d_ids, const float* d_weights, int32_t n_rows,
+                     int32_t d_model, int32_t n_experts, int32_t top_k, int32_t expert_ffn,
+                     const int8_t* d_w_gu, const float* d_s_gu, const int8_t* d_w_down, const float* d_s_down,
+                     void* d_out, int32_t epilogue, void* d_workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,6 +11,7 @@ DARTS_OK, DARTS_EINVAL, DARTS_ENOMEM, DARTS_ESTATE, DARTS_EHIP = 0, 1, 2, 3, 4
 DARTS_F32, DARTS_BF16 = 0, 1
 FLAG_NO_ABORT, FLAG_PERMUTE_PAGES, FLAG_TIMING, FLAG_SHARED_PREFIX, FLAG_STEP_TIMES = 0x1, 0x2, 0x4, 0x8, 0x10
 FLAG_STREAM = 0x20
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 lib_path = os.path.join(_HERE, "libdarts.so")
@@ -105,6 +106,15 @@ _SIGS = {
     "darts_debug_gemm_plan": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P]),
     "darts_gemm": (C.c_int, [_P, _P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                              _P, C.c_size_t, _P]),
+    "darts_moe_route": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, C.c_int32,
+                                  C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_float, _P, _P, _P]),
+    "darts_quantize_rows": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P]),
+    "darts_gemm_i8_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
+    "darts_gemm_i8": (C.c_int, [_P, _P, _P, _P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P,
+                                C.c_size_t, _P]),
+    "darts_moe_ffn_i8_workspace_bytes": (C.c_size_t, [C.c_int32] * 5),
+    "darts_moe_ffn_i8": (C.c_int, [_P, _P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, _P,
+                                   _P, _P, _P, C.c_int32, _P, C.c_size_t, _P]),
     "darts_select_groups": (C.c_int, [_P, _P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                       C.c_int32, C.c_int32, _P, _P, _P, _P, _P, _P, _P, _P]),
 }
@@ -246,6 +256,53 @@ def darts_gemm(a, w, c, M, N, K, dtype, epilogue, workspace=None, stream=None):
     wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(load_library().darts_gemm(_ptr(a), _ptr(w), _ptr(c), M, N, K, dtype, epilogue,
                                      _ptr(workspace), wb, _stream(stream)))
+
+
+def _rows_of(x):
+    """(rows, columns, elements from one row to the next) of a matrix whose rows are contiguous."""
+    rows, cols = x.shape
+    if cols > 1 and x.stride(1) != 1:
+        raise ValueError("the elements of a row must be adjacent")
+    return rows, cols, x.stride(0) if rows > 1 else cols
+
+
+def darts_moe_route(logits, dtype, ids, weights, score=SCORE_SOFTMAX, bias=None, n_groups=1, top_groups=1,
+                    group_best=1, renorm=True, factor=1.0, stream=None):
+    """logits [n_rows, n_experts] (rows may be strided); ids int32 and weights float32 [n_rows, top_k], written."""
+    n_rows, n_experts, ld = _rows_of(logits)
+    _check(load_library().darts_moe_route(_ptr(logits), ld, n_rows, n_experts, dtype, score, _ptr(bias), n_groups,
+                                          top_groups, group_best, ids.shape[1], int(renorm), factor, _ptr(ids),
+                                          _ptr(weights), _stream(stream)))
+
+
+def darts_quantize_rows(x, dtype, q, scale, stream=None):
+    """x [rows, cols] (rows may be strided); q int8 [rows, cols] and scale float32 [rows], written."""
+    rows, cols, ldx = _rows_of(x)
+    _check(load_library().darts_quantize_rows(_ptr(x), ldx, rows, cols, dtype, _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def darts_gemm_i8_workspace_bytes(M, N, K):
+    return int(load_library().darts_gemm_i8_workspace_bytes(M, N, K))
+
+
+def darts_gemm_i8(a, a_scale, w, w_scale, c, M, N, K, epilogue, workspace=None, stream=None):
+    wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(load_library().darts_gemm_i8(_ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(c), M, N, K, epilogue,
+                                        _ptr(workspace) if wb else None, wb, _stream(stream)))
+
+
+def darts_moe_ffn_i8_workspace_bytes(n_rows, d_model, n_experts, top_k, expert_ffn):
+    return int(load_library().darts_moe_ffn_i8_workspace_bytes(n_rows, d_model, n_experts, top_k, expert_ffn))
+
+
+def darts_moe_ffn_i8(x, ids, weights, n_experts, expert_ffn, w_gu, s_gu, w_down, s_down, out, epilogue, workspace,
+                     stream=None):
+    """x [n_rows, d_model] bf16; ids, weights [n_rows, top_k]; out bf16 (epilogue 1) or float32, added to (2)."""
+    n_rows, d_model = x.shape
+    _check(load_library().darts_moe_ffn_i8(_ptr(x), _ptr(ids), _ptr(weights), n_rows, d_model, n_experts,
+                                           ids.shape[1], expert_ffn, _ptr(w_gu), _ptr(s_gu), _ptr(w_down),
+                                           _ptr(s_down), _ptr(out), epilogue, _ptr(workspace),
+                                           workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def darts_debug_gemm_plan(M, N, K, epilogue):

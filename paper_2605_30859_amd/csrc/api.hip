@@ -1375,4 +1375,89 @@ int darts_select_groups(uint8_t* d_status, const int32_t* d_len, const float* d_
   return e == hipSuccess ? DARTS_OK : DARTS_EHIP;
 }
 
+// ------------------------------------------- routing, 8-bit integer layers
+
+static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+int darts_moe_route(const void* d_logits, int64_t ld, int32_t n_rows, int32_t n_experts, int32_t dtype,
+                    int32_t score, const float* d_bias, int32_t n_groups, int32_t top_groups,
+                    int32_t group_best, int32_t top_k, int32_t renorm, float factor, int32_t* d_ids,
+                    float* d_weights, void* stream) {
+  if (n_rows < 0 || n_experts < 1 || n_experts > 1024 || top_k < 1 || top_k > 64 || top_k > n_experts ||
+      ld < n_experts)
+    return DARTS_EINVAL;
+  if (dtype != DARTS_F32 && dtype != DARTS_BF16) return DARTS_EINVAL;
+  if (score != DARTS_SCORE_SOFTMAX && score != DARTS_SCORE_SIGMOID) return DARTS_EINVAL;
+  if (n_groups < 1 || n_groups > 64 || n_experts % n_groups || top_groups < 1 || top_groups > n_groups ||
+      group_best < 1 || group_best > 2 || !std::isfinite(factor))
+    return DARTS_EINVAL;
+  if (n_rows == 0) return DARTS_OK;
+  if (!d_logits || !d_ids || !d_weights) return DARTS_EINVAL;
+  const RouteArgs a{d_logits, ld, n_rows, n_experts, dtype == DARTS_BF16, score == DARTS_SCORE_SIGMOID, d_bias,
+                    n_groups, top_groups, group_best, top_k, renorm != 0, factor, d_ids, d_weights};
+  return launch_route(a, (hipStream_t)stream) == hipSuccess ? DARTS_OK : DARTS_EHIP;
+}
+
+int darts_quantize_rows(const void* d_x, int64_t ldx, int32_t rows, int32_t cols, int32_t dtype, int8_t* d_q,
+                        float* d_scale, void* stream) {
+  if (rows < 0 || cols < 1 || ldx < cols) return DARTS_EINVAL;
+  if (dtype != DARTS_F32 && dtype != DARTS_BF16) return DARTS_EINVAL;
+  if (rows == 0) return DARTS_OK;
+  if (!d_x || !d_q || !d_scale) return DARTS_EINVAL;
+  hipError_t e = launch_quantize_rows(d_x, rows, cols, ldx, dtype == DARTS_BF16, d_q, d_scale, (hipStream_t)stream);
+  return e == hipSuccess ? DARTS_OK : DARTS_EHIP;
+}
+
+constexpr int kI8MaxK = 131072;   // 127 * 127 * 131072 < 2^31
+constexpr int64_t kI8MaxPairs = (int64_t)65535 * kGroupedTileRowsMin;   // an expert's row tiles fit 16 bits
+
+size_t darts_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K) {
+  if (M < 1 || N < 1 || K < 1) return 0;
+  return gemm_i8_workspace_bytes(M, N, K);
+}
+
+int darts_gemm_i8(const int8_t* d_a, const float* d_a_scale, const int8_t* d_w, const float* d_w_scale,
+                  void* d_c, int32_t M, int32_t N, int32_t K, int32_t epilogue, void* d_workspace,
+                  size_t workspace_bytes, void* stream) {
+  if (M < 0 || N < 1 || K < 1 || N % 16 || K % 16 || K > kI8MaxK) return DARTS_EINVAL;
+  if (epilogue < 0 || epilogue > 3 || (epilogue == 3 && N % 32)) return DARTS_EINVAL;
+  if (M == 0) return DARTS_OK;
+  if (!d_a || !d_a_scale || !d_w || !d_w_scale || !d_c) return DARTS_EINVAL;
+  if (!aligned16(d_a) || !aligned16(d_w) || !aligned16(d_workspace)) return DARTS_EINVAL;
+  const size_t need = gemm_i8_workspace_bytes(M, N, K);
+  if (need > workspace_bytes || (need && !d_workspace)) return DARTS_EINVAL;
+  hipError_t e = launch_gemm_i8(d_a, d_a_scale, d_w, d_w_scale, d_c, M, N, K, epilogue, d_workspace, workspace_bytes,
+                                (hipStream_t)stream);
+  return e == hipSuccess ? DARTS_OK : DARTS_EHIP;
+}
+
+static bool ffn_i8_sizes(int32_t n_rows, int32_t d, int32_t E, int32_t k, int32_t Fe) {
+  return n_rows >= 0 && d >= 16 && d % 16 == 0 && d <= kI8MaxK && Fe >= 16 && Fe % 16 == 0 && Fe <= kI8MaxK &&
+         E >= 1 && E <= 1024 && k >= 1 && k <= 64 && (int64_t)n_rows * k <= kI8MaxPairs;
+}
+
+size_t darts_moe_ffn_i8_workspace_bytes(int32_t n_rows, int32_t d_model, int32_t n_experts, int32_t top_k,
+                                        int32_t expert_ffn) {
+  if (n_rows < 1 || !ffn_i8_sizes(n_rows, d_model, n_experts, top_k, expert_ffn)) return 0;
+  return moe_ffn_i8_workspace_bytes(n_rows, d_model, n_experts, top_k, expert_ffn);
+}
+
+int darts_moe_ffn_i8(const void* d_x, const int32_t* d_ids, const float* d_weights, int32_t n_rows,
+                     int32_t d_model, int32_t n_experts, int32_t top_k, int32_t expert_ffn,
+                     const int8_t* d_w_gu, const float* d_s_gu, const int8_t* d_w_down, const float* d_s_down,
+                     void* d_out, int32_t epilogue, void* d_workspace, size_t workspace_bytes, void* stream) {
+  if (!ffn_i8_sizes(n_rows, d_model, n_experts, top_k, expert_ffn)) return DARTS_EINVAL;
+  if (epilogue != 1 && epilogue != 2) return DARTS_EINVAL;
+  if (n_rows == 0) return DARTS_OK;
+  if (!d_x || !d_ids || !d_weights || !d_w_gu || !d_s_gu || !d_w_down || !d_s_down || !d_out || !d_workspace)
+    return DARTS_EINVAL;
+  if (!aligned16(d_x) || !aligned16(d_w_gu) || !aligned16(d_w_down) || !aligned16(d_out) ||
+      ((uintptr_t)d_workspace & 255))
+    return DARTS_EINVAL;
+  if (workspace_bytes < moe_ffn_i8_workspace_bytes(n_rows, d_model, n_experts, top_k, expert_ffn)) return DARTS_EINVAL;
+  const FfnI8Args a{d_x, d_ids, d_weights, n_rows, d_model, n_experts, top_k, expert_ffn, d_w_gu, d_s_gu, d_w_down,
+                    d_s_down, d_out, epilogue == 1 ? EPI_BF16 : EPI_ADD_F32, d_workspace, workspace_bytes};
+  return launch_moe_ffn_i8(a, (hipStream_t)stream) == hipSuccess ? DARTS_OK : DARTS_EHIP;
+}
+
 }  // extern "C"

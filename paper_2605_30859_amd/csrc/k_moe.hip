@@ -198,7 +198,10 @@ __device__ __forceinline__ void moe_place(const int32_t* __restrict__ topk_id, i
                                           int32_t* __restrict__ row_of) {
   for (int i = beg + (int)threadIdx.x; i < end; i += 1024) {
     const int e = topk_id[i];
-    if (e < 0 || e >= E) continue;
+    if (e < 0 || e >= E) {
+      pos_of[i] = -1;
+      continue;
+    }
     const int p = atomicAdd(&cursor[e], 1);
     pos_of[i] = p;
     row_of[p] = i / k;
@@ -364,6 +367,21 @@ __global__ void __launch_bounds__(256) moe_combine_kernel(const bf16_t* __restri
   }
 }
 
+hipError_t launch_moe_lists(const MoeListArgs& a, hipStream_t st) {
+  const MoeLists lists{a.counts, a.offsets, a.mtiles, a.n_mtiles, a.mtiles_dn, a.n_mtiles_dn, a.touched_out,
+                       a.tile_rows, a.tile_rows_dn};
+  if (a.n_pairs <= kMoeOneBlockPairs) {
+    hipLaunchKernelGGL(moe_offsets_kernel, dim3(1), dim3(1024), 0, st, a.topk_id, a.n_pairs, a.E, a.k, lists, a.pos_of,
+                       a.row_of);
+  } else {
+    hipLaunchKernelGGL(moe_count_kernel, dim3(kMoeBlocks), dim3(1024), 0, st, a.topk_id, a.n_pairs, a.E, a.blk);
+    hipLaunchKernelGGL(moe_scan_kernel, dim3(1), dim3(1024), 0, st, a.E, lists, a.blk);
+    hipLaunchKernelGGL(moe_place_kernel, dim3(kMoeBlocks), dim3(1024), 0, st, a.topk_id, a.n_pairs, a.E, a.k, a.blk,
+                       a.pos_of, a.row_of);
+  }
+  return hipGetLastError();
+}
+
 hipError_t launch_moe_ffn(const MoeArgs& a, hipStream_t st, bool* normed) {
   *normed = false;
   if (a.n_rows <= 0) return hipSuccess;
@@ -397,18 +415,10 @@ hipError_t launch_moe_ffn(const MoeArgs& a, hipStream_t st, bool* normed) {
     DARTS_TOPK(kMoeMaxPerLane)
   }
 #undef DARTS_TOPK
-  const MoeLists lists{a.counts, a.offsets, a.mtiles, a.n_mtiles, a.mtiles_dn, a.n_mtiles_dn, a.touched_out,
-                       plan_gu.tile_rows, plan_dn.tile_rows};
-  const int n_pairs = a.n_rows * a.k;
-  if (n_pairs <= kMoeOneBlockPairs) {
-    hipLaunchKernelGGL(moe_offsets_kernel, dim3(1), dim3(1024), 0, st, a.topk_id, n_pairs, a.E, a.k, lists, a.pos_of,
-                       a.row_of);
-  } else {
-    hipLaunchKernelGGL(moe_count_kernel, dim3(kMoeBlocks), dim3(1024), 0, st, a.topk_id, n_pairs, a.E, a.blk);
-    hipLaunchKernelGGL(moe_scan_kernel, dim3(1), dim3(1024), 0, st, a.E, lists, a.blk);
-    hipLaunchKernelGGL(moe_place_kernel, dim3(kMoeBlocks), dim3(1024), 0, st, a.topk_id, n_pairs, a.E, a.k, a.blk,
-                       a.pos_of, a.row_of);
-  }
+  const MoeListArgs lists{a.topk_id, a.n_rows * a.k, a.E, a.k, a.counts, a.offsets, a.mtiles, a.n_mtiles, a.mtiles_dn,
+                          a.n_mtiles_dn, plan_gu.tile_rows, plan_dn.tile_rows, a.touched_out, a.blk, a.pos_of,
+                          a.row_of};
+  if ((e = launch_moe_lists(lists, st)) != hipSuccess) return e;
   const int Fe = a.Fe, d = a.d;
   // gate/up: N = 2*Fe, K = d (SwiGLU into h_perm), A rows gathered from xn;
   // down: N = d, K = Fe

@@ -273,5 +273,41 @@ struct MoeArgs {
 };
 // *normed: the combine also wrote xn = bf16(RMSNorm(x)) (d <= 4096)
 hipError_t launch_moe_ffn(const MoeArgs& a, hipStream_t st, bool* normed);
+// The routing lists of n_pairs (row, slot) pairs (fields as in MoeArgs; pos_of is
+// -1 for a pair whose id lies outside [0, E)).
+struct MoeListArgs {
+  const int32_t* topk_id; int n_pairs, E, k;
+  int32_t *counts, *offsets, *mtiles, *n_mtiles, *mtiles_dn, *n_mtiles_dn;
+  int tile_rows, tile_rows_dn;
+  int32_t* touched_out;
+  int32_t *blk, *pos_of, *row_of;
+};
+hipError_t launch_moe_lists(const MoeListArgs& a, hipStream_t st);
+
+// ---- routing to experts (k_route.hip)
+struct RouteArgs {
+  const void* logits; int64_t ld; int64_t n_rows; int n_experts; bool bf16;
+  bool sigmoid; const float* bias;
+  int n_groups, top_groups, group_best, top_k; bool renorm; float factor;
+  int32_t* ids; float* weights;
+};
+hipError_t launch_route(const RouteArgs& a, hipStream_t st);
+
+// ---- 8-bit integers (k_i8.hip)
+hipError_t launch_quantize_rows(const void* x, int64_t rows, int cols, int64_t ldx, bool bf16, int8_t* q, float* scale,
+                                hipStream_t st);
+size_t gemm_i8_workspace_bytes(int M, int N, int K);
+hipError_t launch_gemm_i8(const int8_t* a, const float* a_scale, const int8_t* w, const float* w_scale, void* c, int M,
+                          int N, int K, int epi, void* ws, size_t ws_bytes, hipStream_t st);
+size_t moe_ffn_i8_workspace_bytes(int64_t rows, int d, int E, int k, int Fe);
+struct FfnI8Args {
+  const void* x; const int32_t* ids; const float* weights;   // [n_rows][d] bf16, [n_rows][k]
+  int n_rows, d, E, k, Fe;
+  const int8_t* w_gu; const float* s_gu;       // [E][2Fe][d], gate/up rows interleaved in groups of 16
+  const int8_t* w_down; const float* s_down;   // [E][d][Fe]
+  void* out; int epi;                          // EPI_BF16 or EPI_ADD_F32
+  void* ws; size_t ws_bytes;
+};
+hipError_t launch_moe_ffn_i8(const FfnI8Args& a, hipStream_t st);
 
 }  // namespace darts
