@@ -9,13 +9,13 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "common.h"
+#include "gemm_tiles.h"
 #include "kernels.h"
 
 namespace darts {
-
-typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------ rows to codes
 // The magnitude is found on the bits without the sign, whose order as integers
@@ -35,157 +35,572 @@ __device__ __forceinline__ int code_of(float x, float up) {
   return up == 0.f ? 0 : (int)__builtin_rintf(x * up);
 }
 
+// Eight elements of a row as float32, and eight codes.
+template <bool BF16>
+struct X8;
+template <>
+struct X8<true> {
+  u32x4_t v;
+  __device__ __forceinline__ void load(const void* x, int64_t i) { v = *(const u32x4_t*)((const bf16_t*)x + i); }
+  __device__ __forceinline__ float at(int e) const {
+    return __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16);
+  }
+};
+template <>
+struct X8<false> {
+  f32x4_t v[2];
+  __device__ __forceinline__ void load(const void* x, int64_t i) {
+    v[0] = *(const f32x4_t*)((const float*)x + i);
+    v[1] = *(const f32x4_t*)((const float*)x + i + 4);
+  }
+  __device__ __forceinline__ float at(int e) const { return v[e >> 2][e & 3]; }
+};
 template <bool BF16>
 __device__ __forceinline__ float load_x(const void* x, int64_t i) {
   return BF16 ? bf16_to_f32(((const bf16_t*)x)[i]) : ((const float*)x)[i];
 }
-
-// One block of 256 threads per row.
-template <bool BF16>
-__global__ void __launch_bounds__(256) quantize_rows_kernel(const void* __restrict__ x, int cols, int64_t ldx,
-                                                            int8_t* __restrict__ q, float* __restrict__ scale) {
-  __shared__ uint32_t red[4];
-  const int64_t r = blockIdx.x;
-  uint32_t top = 0;
-  for (int c = threadIdx.x; c < cols; c += 256)
-    top = max(top, __float_as_uint(load_x<BF16>(x, r * ldx + c)) & 0x7fffffffu);
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
-  __syncthreads();
-  top = max(max(red[0], red[1]), max(red[2], red[3]));
-  float up, sc;
-  row_scale(top, up, sc);
-  if (threadIdx.x == 0) scale[r] = sc;
-  for (int c = threadIdx.x; c < cols; c += 256) q[r * cols + c] = (int8_t)code_of(load_x<BF16>(x, r * ldx + c), up);
+  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+  return v;
 }
 
-hipError_t launch_quantize_rows(const void* x, int64_t rows, int cols, int64_t ldx, bool bf16, int8_t* q, float* scale,
-                                hipStream_t st) {
-  for (int64_t r = 0; r < rows; r += INT32_MAX / 256) {
-    const dim3 grid((unsigned)std::min<int64_t>(rows - r, INT32_MAX / 256));
-    const char* xr = (const char*)x + r * ldx * (bf16 ? 2 : 4);
-    if (bf16) hipLaunchKernelGGL(quantize_rows_kernel<true>, grid, dim3(256), 0, st, xr, cols, ldx, q + r * cols, scale + r);
-    else hipLaunchKernelGGL(quantize_rows_kernel<false>, grid, dim3(256), 0, st, xr, cols, ldx, q + r * cols, scale + r);
+// WPR wavefronts per row, blocks of four.  VEC: rows of whole 16-byte pieces; the
+// first kQuantKeep pieces of a lane stay in registers between the two passes, so
+// rows of up to 64 * WPR * 32 elements are read once.
+constexpr int kQuantKeep = 4;
+template <bool BF16, bool VEC, int WPR>
+__global__ void __launch_bounds__(256) quantize_rows_kernel(const void* __restrict__ x, int64_t rows, int cols, int64_t ldx,
+                                                            int8_t* __restrict__ q, float* __restrict__ scale) {
+  __shared__ uint32_t red[4];
+  constexpr int T = 64 * WPR;                          // threads of a row
+  const int64_t r = (int64_t)blockIdx.x * (4 / WPR) + threadIdx.x / T;
+  const int t = threadIdx.x % T;
+  if (WPR == 1 && r >= rows) return;
+  X8<BF16> keep[kQuantKeep];
+  uint32_t top = 0;
+  const int n8 = cols / 8;
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < kQuantKeep; ++i)
+      if (t + T * i < n8) keep[i].load(x, r * ldx + (t + T * i) * 8);
+#pragma unroll
+    for (int i = 0; i < kQuantKeep; ++i)
+      if (t + T * i < n8)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(keep[i].at(e)) & 0x7fffffffu);
+    for (int c = t + T * kQuantKeep; c < n8; c += T) {
+      X8<BF16> v;
+      v.load(x, r * ldx + c * 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v.at(e)) & 0x7fffffffu);
+    }
+  } else {
+    for (int c = t; c < cols; c += T) top = max(top, __float_as_uint(load_x<BF16>(x, r * ldx + c)) & 0x7fffffffu);
+  }
+  top = wave_max_u32(top);
+  if constexpr (WPR == 4) {
+    if ((t & 63) == 0) red[t >> 6] = top;
+    __syncthreads();
+    top = max(max(red[0], red[1]), max(red[2], red[3]));
+  }
+  float up, sc;
+  row_scale(top, up, sc);
+  if (t == 0) scale[r] = sc;
+  auto store = [&](const X8<BF16>& v, int c) {
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      w[h] = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[h] |= ((uint32_t)code_of(v.at(4 * h + e), up) & 0xffu) << (8 * e);
+    }
+    *(uint2*)(q + r * cols + c * 8) = make_uint2(w[0], w[1]);
+  };
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < kQuantKeep; ++i)
+      if (t + T * i < n8) store(keep[i], t + T * i);
+    for (int c = t + T * kQuantKeep; c < n8; c += T) {
+      X8<BF16> v;
+      v.load(x, r * ldx + c * 8);
+      store(v, c);
+    }
+  } else {
+    for (int c = t; c < cols; c += T) q[r * cols + c] = (int8_t)code_of(load_x<BF16>(x, r * ldx + c), up);
+  }
+}
+
+template <bool BF16, bool VEC>
+static hipError_t quantize_go(const void* x, int64_t rows, int cols, int64_t ldx, int8_t* q, float* scale, hipStream_t st) {
+  // a wavefront per row where it holds the row, and there are rows for every CU
+  const int wpr = cols <= 64 * 8 * kQuantKeep && rows >= 2048 ? 1 : 4;
+  const int64_t most = (int64_t)(1 << 22) * (4 / wpr);       // rows per launch
+  for (int64_t r = 0; r < rows; r += most) {
+    const int64_t n = std::min(rows - r, most);
+    const dim3 grid((unsigned)((n * wpr + 3) / 4));
+    const char* xr = (const char*)x + r * ldx * (BF16 ? 2 : 4);
+    if (wpr == 1)
+      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 1>), grid, dim3(256), 0, st, xr, n, cols, ldx, q + r * cols, scale + r);
+    else
+      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 4>), grid, dim3(256), 0, st, xr, n, cols, ldx, q + r * cols, scale + r);
   }
   return hipGetLastError();
 }
 
-// ------------------------------------------------------------------ products
-__device__ __forceinline__ float silu_i8(float g) { return g / (1.0f + __expf(-g)); }
-
-// What a tile of a product reads and writes.
-struct I8Tile {
-  const int8_t *a, *w;            // rows of K codes
-  const float *a_scale, *w_scale;
-  void* c;
-  int rows, N, K, ldc;            // rows of the product; channels
-  const int32_t* arow;            // NULL, or the row of a (and a_scale) of each of them
-};
-
-template <int EPI>
-__device__ __forceinline__ void store_i8(void* c, int64_t at, float v) {
-  if (EPI == EPI_F32) ((float*)c)[at] = v;
-  else if (EPI == EPI_ADD_F32) ((float*)c)[at] += v;
-  else ((bf16_t*)c)[at] = f32_to_bf16(v);
+hipError_t launch_quantize_rows(const void* x, int64_t rows, int cols, int64_t ldx, bool bf16, int8_t* q, float* scale,
+                                hipStream_t st) {
+  const bool vec = cols % 8 == 0 && ((uintptr_t)x & 15) == 0 && ((uintptr_t)q & 7) == 0 && ldx * (bf16 ? 2 : 4) % 16 == 0;
+  if (bf16) return vec ? quantize_go<true, true>(x, rows, cols, ldx, q, scale, st)
+                       : quantize_go<true, false>(x, rows, cols, ldx, q, scale, st);
+  return vec ? quantize_go<false, true>(x, rows, cols, ldx, q, scale, st)
+             : quantize_go<false, false>(x, rows, cols, ldx, q, scale, st);
 }
 
-// A 64 x 64 tile by four wavefronts of 16 rows each; operands go straight from
-// memory into the matrix instructions' registers.  Codes past K are zero, rows
-// past the last repeat it and are not stored.
-template <int EPI>
-__device__ __forceinline__ void i8_tile(const I8Tile& t, int m0, int n0) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, fr = lane & 15, fq = lane >> 4;
-  int row = min(m0 + 16 * w + fr, t.rows - 1);
-  if (t.arow) row = t.arow[row];
-  const int8_t* a = t.a + (int64_t)row * t.K;
-  const int8_t* b[4];
+// ------------------------------------------------------------------ products
+// The kernels of the bf16 products on codes (gemm_tiles.h): a 16-byte chunk holds
+// 16 codes where it held 8 bf16, so the same tiles, LDS layouts and loads feed
+// v_mfma_i32_16x16x64_i8, which takes as long as v_mfma_f32_16x16x32_bf16 and does
+// twice the products.  K2 = K / 2 is K in the 16-bit units of those kernels.
+//  * skinny (few rows): operands go straight from memory into registers, 8
+//    wavefronts of a block split K and are added through LDS;
+//  * ring: tiles through a ring of LDS stages;
+//  * alternating groups (many rows): 256-row tiles on persistent blocks.
+// The last two may split K over blocks: the partial sums are integers in a
+// workspace, so neither the plan nor the order changes any result.
+
+// Up to 16 * MT rows.  WK wavefronts share a strip of 16 channels, each a range of
+// kw codes of K (a multiple of 64), and a block has 8 / WK strips.  Lane (r, q)
+// loads 16 codes of row r; the loads of U steps of 64 are issued before the
+// products of the U steps before.
+template <int MT, int WK, int EPI>
+__global__ void __launch_bounds__(512) gemm_i8_skinny_kernel(const int8_t* __restrict__ A, const float* __restrict__ a_scale,
+                                                             const int8_t* __restrict__ W, const float* __restrict__ w_scale,
+                                                             void* __restrict__ C, int ldc, int M, int N, int K, int kw) {
+  constexpr int U = 4, NS = 8 / WK;
+  static_assert(EPI != EPI_SWIGLU || NS % 2 == 0, "gate and up strips in one block");
+  __shared__ i32x4_t red[8][MT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, fq = lane >> 4;
+  const int strip = blockIdx.x * NS + wave / WK;
+  const int kb = (wave % WK) * kw, ke = min(K, kb + kw);
+  i32x4_t acc[MT];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) b[j] = t.w + (int64_t)min(n0 + 16 * j + fr, t.N - 1) * t.K;
-  i32x4_t acc[4];
+  for (int i = 0; i < MT; ++i) acc[i] = (i32x4_t){0, 0, 0, 0};
+  const int8_t* wp = W + (int64_t)min(strip * 16 + fr, N - 1) * K;
+  const int8_t* ap[MT];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) acc[j] = (i32x4_t){0, 0, 0, 0};
-  for (int k = 16 * fq; k < ((t.K + 63) & ~63); k += 64) {
-    i32x4_t x = {0, 0, 0, 0}, y[4];
+  for (int i = 0; i < MT; ++i) ap[i] = A + (int64_t)min(16 * i + fr, M - 1) * K;
+  i32x4_t a[2][U][MT], b[2][U];
+  auto load = [&](int k, int p) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = x;
-    if (k < t.K) {
-      x = *(const i32x4_t*)(a + k);
+    for (int u = 0; u < U; ++u) {
+      const int at = min(k + 64 * u + 16 * fq, ke - 16);
+      b[p][u] = __builtin_nontemporal_load((const i32x4_t*)(wp + at));
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = *(const i32x4_t*)(b[j] + k);
+      for (int i = 0; i < MT; ++i) a[p][u][i] = *(const i32x4_t*)(ap[i] + at);
     }
+  };
+  auto mma = [&](int k, int p) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, y[j], acc[j], 0, 0, 0);
-  }
-  // lane: rows 4 * (lane / 16) + i, column lane % 16
+    for (int u = 0; u < U; ++u) {
+      const bool in = k + 64 * u + 16 * fq < ke;       // past the end: W's last codes against zeros
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int m = m0 + 16 * w + 4 * fq + i;
-    if (m >= t.rows) continue;
-    const float sa = t.a_scale[t.arow ? t.arow[m] : m];
-#pragma unroll
-    for (int j = 0; j < 4; j += EPI == EPI_SWIGLU ? 2 : 1) {
-      const int n = n0 + 16 * j + fr;
-      if (n >= t.N) continue;
-      const float v = (float)acc[j][i] * sa * t.w_scale[n];
-      if constexpr (EPI == EPI_SWIGLU) {
-        const float u = (float)acc[j + 1][i] * sa * t.w_scale[n + 16];
-        store_i8<EPI_BF16>(t.c, (int64_t)m * t.ldc + (n >> 5) * 16 + fr, silu_i8(v) * u);
-      } else {
-        store_i8<EPI>(t.c, (int64_t)m * t.ldc + n, v);
+      for (int i = 0; i < MT; ++i) {
+        if (!in) a[p][u][i] = (i32x4_t){0, 0, 0, 0};
+        acc[i] = I8Op::mma(a[p][u][i], b[p][u], acc[i]);
       }
     }
-  }
-}
-
-template <int EPI>
-__global__ void __launch_bounds__(256) gemm_i8_kernel(I8Tile t, int mt) {
-  i8_tile<EPI>(t, (int)(blockIdx.x % mt) * 64, (int)(blockIdx.x / mt) * 64);
-}
-
-// Expert e owns rows [off[e], off[e] + cnt[e]) of C, and of A or of the row list
-// into A; mtiles lists the non-empty row tiles.
-struct I8Groups {
-  const int32_t *off, *cnt, *mtiles, *n_mtiles;
-};
-template <int EPI>
-__global__ void __launch_bounds__(256) gemm_i8_grouped_kernel(I8Tile t, I8Groups g, int nt) {
-  const int total = g.n_mtiles[0] * nt;
-  for (int it = blockIdx.x; it < total; it += gridDim.x) {
-    const int mt = g.mtiles[it / nt], e = mt >> 16;
-    const int64_t off = g.off[e];
-    I8Tile u = t;
-    if (t.arow) {
-      u.arow = t.arow + off;
-    } else {
-      u.a = t.a + off * t.K;
-      u.a_scale = t.a_scale + off;
+  };
+  if (kb < ke) {
+    load(kb, 0);
+    for (int k = kb; k < ke; k += 2 * 64 * U) {
+      if (k + 64 * U < ke) load(k + 64 * U, 1);
+      mma(k, 0);
+      if (k + 64 * U >= ke) break;
+      if (k + 2 * 64 * U < ke) load(k + 2 * 64 * U, 0);
+      mma(k + 64 * U, 1);
     }
-    u.w = t.w + (int64_t)e * t.N * t.K;
-    u.w_scale = t.w_scale + (int64_t)e * t.N;
-    u.c = (char*)t.c + off * t.ldc * (EPI == EPI_F32 || EPI == EPI_ADD_F32 ? 4 : 2);
-    u.rows = g.cnt[e];
-    i8_tile<EPI>(u, (mt & 0xffff) * 64, it % nt * 64);
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) red[wave][i][lane] = acc[i];
+  __syncthreads();
+  // wavefront t adds and stores tile t (SwiGLU: gate and up)
+  constexpr int P = EPI == EPI_SWIGLU ? 2 : 1;
+  for (int t = wave; t < MT * NS / P; t += 8) {
+    const int i = t / (NS / P), s0 = t % (NS / P) * P;
+    i32x4_t s[1][P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      s[0][p] = red[(s0 + p) * WK][i][lane];
+#pragma unroll
+      for (int w = 1; w < WK; ++w) s[0][p] += red[(s0 + p) * WK + w][i][lane];
+    }
+    const I8Op::Extra ex{a_scale, w_scale, 0};
+    store_i8_tiles<1, P, EPI, false>(C, ldc, M, N, i * 16, (blockIdx.x * NS + s0) * 16, lane, s, ex);
   }
 }
 
-size_t gemm_i8_workspace_bytes(int, int, int) { return 0; }
+template <int BM, int BN, int WGM, int WGN, int STAGES, int EPI, bool SPLIT, int WAUX>
+__global__ void __launch_bounds__(64 * WGM * WGN)
+    gemm_i8_ring_kernel(const int8_t* __restrict__ A, const float* __restrict__ a_scale, const int8_t* __restrict__ W,
+                        const float* __restrict__ w_scale, void* __restrict__ C, int ldc, int M, int N, int K2, int k_chunk,
+                        int mt, int nt, int32_t* __restrict__ ws) {
+  const int b = xcd_block();
+  const int mi = b % mt, ni = (b / mt) % nt, z = b / (mt * nt);
+  const I8Op::Extra ex{a_scale, w_scale, min(k_chunk, K2 - z * k_chunk)};
+  dma_gemm_tile<I8Op, BM, BN, 64, WGM, WGN, STAGES, EPI, SPLIT, false, WAUX>(
+      (const bf16_t*)A, K2, (const bf16_t*)W, K2, C, ldc, M, N, k_chunk, mi, ni, z, (float*)ws, nullptr, ex);
+}
+
+// One persistent block per CU, each XCD a contiguous eighth of the tiles.
+template <int BM, int BN, int WGM, int WGN, int EPI, bool SPLIT>
+__global__ void __launch_bounds__(512, 2)
+    gemm_i8_alt_kernel(const int8_t* __restrict__ A, const float* __restrict__ a_scale, const int8_t* __restrict__ W,
+                       const float* __restrict__ w_scale, void* __restrict__ C, int ldc, int M, int N, int K2, int k_chunk,
+                       int mt, int nt, int n_split, int32_t* __restrict__ ws) {
+  constexpr int esz = (SPLIT || EPI == EPI_F32 || EPI == EPI_ADD_F32) ? 4 : 2;
+  const int total = mt * nt * n_split, chunk = (total + 7) >> 3;
+  const int hi = min(total, ((int)(blockIdx.x & 7) + 1) * chunk);
+  int it = (int)(blockIdx.x & 7) * chunk + (int)(blockIdx.x >> 3);
+  auto next = [&](AltItem& t) {
+    if (it >= hi) return false;
+    const int z = it / (mt * nt);
+    int mi, ni;
+    panel_order(it - z * mt * nt, mt, nt, mi, ni);
+    it += (int)(gridDim.x >> 3);
+    t.a = (const bf16_t*)A + (int64_t)mi * BM * K2 + z * k_chunk;
+    t.w = (const bf16_t*)W + (int64_t)ni * BN * K2 + z * k_chunk;
+    const int64_t out = (int64_t)mi * BM * ldc + (EPI == EPI_SWIGLU && !SPLIT ? ni * BN / 2 : ni * BN);
+    t.c = SPLIT ? (char*)(ws + (int64_t)z * M * N + out) : (char*)C + out * esz;
+    t.rows = M - mi * BM;
+    t.arow = nullptr;
+    t.a_scale = a_scale + mi * BM;
+    t.w_scale = w_scale + ni * BN;
+    t.cols = N - ni * BN;
+    return true;
+  };
+  alt_gemm_items<I8Op, BM, BN, WGM, WGN, EPI, SPLIT, false>(K2, K2, ldc, k_chunk / 64, next);
+}
+
+// Partial sums of S splits, scales and epilogue; four columns per thread.
+template <int EPI>
+__global__ void __launch_bounds__(256) reduce_i8_kernel(const int32_t* __restrict__ ws, int S, int M, int N,
+                                                        const float* __restrict__ a_scale, const float* __restrict__ w_scale,
+                                                        void* C, int ldc) {
+  const int ncol4 = (EPI == EPI_SWIGLU ? N / 2 : N) / 4;
+  const int64_t total = (int64_t)M * ncol4, zs = (int64_t)M * N;
+  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
+    const int m = (int)(t / ncol4), c = (int)(t % ncol4) * 4;
+    const int n = EPI == EPI_SWIGLU ? (c >> 4) * 32 + (c & 15) : c;
+    const float sa = a_scale[m];
+    auto value = [&](int col, float (&v)[4]) {
+      i32x4_t s = {0, 0, 0, 0};
+      for (int z = 0; z < S; ++z) s += *(const i32x4_t*)(ws + z * zs + (int64_t)m * N + col);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (float)s[e] * sa * w_scale[col + e];
+    };
+    float v[4];
+    value(n, v);
+    if constexpr (EPI == EPI_SWIGLU) {
+      float u[4];
+      value(n + 16, u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = silu_f(v[e]) * u[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) epi_store<EPI == EPI_SWIGLU ? EPI_BF16 : EPI>(C, ldc, M, m, c + e, v[e]);
+  }
+}
+
+// ------------------------------------------------------------------ dispatch
+// A plan: the kernel, its tiles and K splits; a function of (M, N, K) alone.
+struct I8Plan {
+  int kind;          // index into kI8Tiles, or -1 skinny
+  int mt, nt;        // tiles
+  int S;             // K splits (skinny: wavefronts per strip)
+  int k_chunk;       // units per split
+};
+// The tiles, and a model of their times: a block's time is fixed + per_k * (K tiles
+// of 128 codes), in us, with one block per CU; with two on a CU, gain is the CU's
+// speed against one block's.  Fitted to 300 sizes (16 shapes, 16 to 16384 rows,
+// weights from memory): the plans that it gives take 1.4% longer on average than
+// the fastest measured one.
+struct I8Tiles {
+  int bm, bn, occ;
+  bool alt;
+  double fixed, per_k, gain;
+};
+static constexpr I8Tiles kI8Tiles[] = {
+    {64, 64, 2, false, 1.21, 0.320, 1.35},  {64, 128, 2, false, 2.11, 0.493, 1.39}, {128, 128, 2, false, 2.82, 0.897, 1.68},
+    {256, 128, 1, true, 2.63, 0.773, 1.0},  {256, 192, 1, true, 3.37, 1.046, 1.0},  {256, 256, 1, true, 4.02, 1.233, 1.0}};
+constexpr int kI8Kinds = sizeof(kI8Tiles) / sizeof(kI8Tiles[0]);
+constexpr int kI8Cus = 256;
+constexpr double kI8LaunchUs = 3.25, kI8ReduceUs = 2.2;      // of the launch, of the reduce kernel
+constexpr double kI8ReadMBs = 4.94e6, kI8SplitMBs = 5.7e6;   // bytes per us: operands and results, partial sums
+
+static bool set_i8_plan(I8Plan& p, int kind, int S, int M, int N, int K) {
+  const int K2 = K / 2;
+  p.kind = kind;
+  p.S = S;
+  p.mt = p.nt = 0;
+  p.k_chunk = K2;
+  if (kind < 0) return M <= 32 && (S == 4 || S == 8);
+  const I8Tiles& t = kI8Tiles[kind];
+  p.mt = (M + t.bm - 1) / t.bm;
+  p.nt = (N + t.bn - 1) / t.bn;
+  if (t.alt) {
+    // whole pairs of K tiles; 32-bit byte offsets inside a tile
+    if (K2 % (128 * S) || (int64_t)256 * std::max<int64_t>(K, 4 * (int64_t)N) >= ((int64_t)1 << 31)) return false;
+    p.k_chunk = K2 / S;
+  } else {
+    p.k_chunk = (K2 + 64 * S - 1) / (64 * S) * 64;
+    if ((int64_t)p.k_chunk * (S - 1) >= K2) return false;      // a split without work
+  }
+  return (int64_t)p.mt * p.nt * S <= INT32_MAX / 512;
+}
+
+static double i8_estimate(const I8Plan& p, int M, int N, int K) {
+  const I8Tiles& t = kI8Tiles[p.kind];
+  const double blocks = (double)p.mt * p.nt * p.S, tile = t.fixed + t.per_k * ((p.k_chunk + 63) / 64);
+  double us = blocks <= kI8Cus ? tile : std::ceil(blocks / (t.occ * kI8Cus)) * t.occ * tile / t.gain;
+  us = std::max(us, ((double)N * K + (double)M * K + 2.0 * M * N) / kI8ReadMBs) + kI8LaunchUs;
+  if (p.S > 1) us += kI8ReduceUs + 8.0 * p.S * M * N / kI8SplitMBs;
+  return us;
+}
+
+// Skinny: a few rows; up to 16 of them while the weights are small (16 rows: 4096 x
+// 4096 8.0 us against 9.1 in tiles, 6144 x 4096 12.1 against 10.9), up to 32 while
+// K is short, too (32 rows: 8192 x 1024 6.0 against 6.6, 2048 x 4096 9.2 against
+// 8.7).  Eight wavefronts per strip, or four of twice the range where the strips
+// alone give enough of them (one row: 6144 x 4096 8.5 us with four, 9.4 with
+// eight; 2048 x 4096 7.8 and 5.3; 12288 x 8192 25 and 20.7).
+static bool skinny_i8_plan(I8Plan& p, int M, int N, int K) {
+  const int64_t w = (int64_t)N * K;
+  if (M > 4 && !(M <= 16 && w <= 20000000) && !(M <= 32 && w <= 8400000 && K <= 2048)) return false;
+  return set_i8_plan(p, -1, N >= 16 * 384 && K <= 4096 ? 4 : 8, M, N, K);
+}
+
+static I8Plan plan_i8(int M, int N, int K) {
+  I8Plan best, p;
+  if (skinny_i8_plan(best, M, N, K)) return best;
+  double least = 1e300;
+  for (int kind = 0; kind < kI8Kinds; ++kind)
+    for (int S = 1; S <= 8; S *= 2) {
+      if (!set_i8_plan(p, kind, S, M, N, K)) continue;
+      const double us = i8_estimate(p, M, N, K);
+      if (us < least) {
+        least = us;
+        best = p;
+      }
+    }
+  return best;
+}
+
+static size_t plan_ws_bytes(const I8Plan& p, int M, int N) { return p.kind >= 0 && p.S > 1 ? (size_t)p.S * M * N * 4 : 0; }
+size_t gemm_i8_workspace_bytes(int M, int N, int K) { return plan_ws_bytes(plan_i8(M, N, K), M, N); }
+
+// Dynamic LDS beyond 64 KB is allowed once per kernel and device.
+static hipError_t allow_lds(const void* kern, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+  e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
+struct I8Call {
+  const int8_t* a;
+  const float* a_scale;
+  const int8_t* w;
+  const float* w_scale;
+  void* c;
+  int M, N, K, ldc;
+  int32_t* ws;
+};
+
+template <int EPI, int MT, int WK>
+static void skinny_i8_go(const I8Call& c, hipStream_t st) {
+  constexpr int cols = 8 / WK * 16;
+  const int kw = (c.K + WK * 64 - 1) / (WK * 64) * 64;
+  hipLaunchKernelGGL((gemm_i8_skinny_kernel<MT, WK, EPI>), dim3((c.N + cols - 1) / cols), dim3(512), 0, st, c.a,
+                     c.a_scale, c.w, c.w_scale, c.c, c.ldc, c.M, c.N, c.K, kw);
+}
+template <int EPI, int MT>
+static void skinny_i8(int wk, const I8Call& c, hipStream_t st) {
+  if (wk == 4 || EPI == EPI_SWIGLU) skinny_i8_go<EPI, MT, 4>(c, st);
+  else skinny_i8_go<EPI, MT, EPI == EPI_SWIGLU ? 4 : 8>(c, st);
+}
+
+template <int EPI, int BM, int BN, int WGM, int WGN, int ST, bool SPLIT>
+static hipError_t ring_i8_go(const I8Plan& p, const I8Call& c, hipStream_t st) {
+  constexpr int lds = ST * (BM + BN) * 64 * 2;
+  auto kern = gemm_i8_ring_kernel<BM, BN, WGM, WGN, ST, EPI, SPLIT, 0>;
+  static std::atomic<uint64_t> done{0};
+  hipError_t e = allow_lds((const void*)kern, lds, done);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3(p.mt * p.nt * p.S), dim3(64 * WGM * WGN), lds, st, c.a, c.a_scale, c.w, c.w_scale, c.c,
+                     c.ldc, c.M, c.N, c.K / 2, p.k_chunk, p.mt, p.nt, c.ws);
+  return hipGetLastError();
+}
+
+template <int EPI, int BM, int BN, int WGM, int WGN, bool SPLIT>
+static hipError_t alt_i8_go(const I8Plan& p, const I8Call& c, hipStream_t st) {
+  constexpr int lds = 2 * (BM + BN) * 64 * 2 + (SPLIT ? 0 : kAltScaleBytes);
+  auto kern = gemm_i8_alt_kernel<BM, BN, WGM, WGN, EPI, SPLIT>;
+  static std::atomic<uint64_t> done{0};
+  hipError_t e = allow_lds((const void*)kern, lds, done);
+  if (e != hipSuccess) return e;
+  const int blocks = std::min((p.mt * p.nt * p.S + 7) / 8 * 8, kI8Cus);
+  hipLaunchKernelGGL(kern, dim3(blocks), dim3(512), lds, st, c.a, c.a_scale, c.w, c.w_scale, c.c, SPLIT ? c.N : c.ldc, c.M,
+                     c.N, c.K / 2, p.k_chunk, p.mt, p.nt, p.S, c.ws);
+  return hipGetLastError();
+}
+
+template <int EPI, bool SPLIT>
+static hipError_t tiles_i8_go(const I8Plan& p, const I8Call& c, hipStream_t st) {
+  switch (p.kind) {
+    case 0: return ring_i8_go<EPI, 64, 64, 2, 2, 4, SPLIT>(p, c, st);
+    case 1: return ring_i8_go<EPI, 64, 128, 2, 2, 3, SPLIT>(p, c, st);
+    case 2: return ring_i8_go<EPI, 128, 128, 2, 2, 2, SPLIT>(p, c, st);
+    case 3: return alt_i8_go<EPI, 256, 128, 4, 2, SPLIT>(p, c, st);
+    case 4: return alt_i8_go<EPI, 256, 192, 4, 2, SPLIT>(p, c, st);
+    default: return alt_i8_go<EPI, 256, 256, 2, 4, SPLIT>(p, c, st);
+  }
+}
+
+template <int EPI>
+static hipError_t gemm_i8_go(const I8Plan& p, const I8Call& c, hipStream_t st) {
+  if (p.kind < 0) {
+    if (c.M <= 16) skinny_i8<EPI, 1>(p.S, c, st);
+    else skinny_i8<EPI, 2>(p.S, c, st);
+    return hipGetLastError();
+  }
+  if (p.S == 1) return tiles_i8_go<EPI, false>(p, c, st);
+  // partial sums do not depend on the epilogue
+  hipError_t e = tiles_i8_go<EPI_F32, true>(p, c, st);
+  if (e != hipSuccess) return e;
+  const int64_t n4 = (int64_t)c.M * (EPI == EPI_SWIGLU ? c.N / 2 : c.N) / 4;
+  hipLaunchKernelGGL(reduce_i8_kernel<EPI>, dim3((unsigned)std::min<int64_t>((n4 + 255) / 256, 16384)), dim3(256), 0, st,
+                     c.ws, p.S, c.M, c.N, c.a_scale, c.w_scale, c.c, c.ldc);
+  return hipGetLastError();
+}
+
+static hipError_t run_i8_plan(const I8Plan& p, const I8Call& c, int epi, hipStream_t st) {
+  switch (epi) {
+    case EPI_F32: return gemm_i8_go<EPI_F32>(p, c, st);
+    case EPI_BF16: return gemm_i8_go<EPI_BF16>(p, c, st);
+    case EPI_ADD_F32: return gemm_i8_go<EPI_ADD_F32>(p, c, st);
+    case EPI_SWIGLU: return gemm_i8_go<EPI_SWIGLU>(p, c, st);
+  }
+  return hipErrorInvalidValue;
+}
 
 hipError_t launch_gemm_i8(const int8_t* a, const float* a_scale, const int8_t* w, const float* w_scale, void* c, int M,
-                          int N, int K, int epi, void*, size_t, hipStream_t st) {
+                          int N, int K, int epi, void* ws, size_t ws_bytes, hipStream_t st) {
   if (M <= 0) return hipSuccess;
-  const int mt = (M + 63) / 64;
-  const int64_t blocks = (int64_t)mt * ((N + 63) / 64);
-  if (blocks > INT32_MAX / 256) return hipErrorInvalidValue;
-  const I8Tile t{a, w, a_scale, w_scale, c, M, N, K, epi == EPI_SWIGLU ? N / 2 : N, nullptr};
-  const dim3 grid((unsigned)blocks), blk(256);
-  switch (epi) {
-    case EPI_F32: hipLaunchKernelGGL(gemm_i8_kernel<EPI_F32>, grid, blk, 0, st, t, mt); break;
-    case EPI_BF16: hipLaunchKernelGGL(gemm_i8_kernel<EPI_BF16>, grid, blk, 0, st, t, mt); break;
-    case EPI_ADD_F32: hipLaunchKernelGGL(gemm_i8_kernel<EPI_ADD_F32>, grid, blk, 0, st, t, mt); break;
-    case EPI_SWIGLU: hipLaunchKernelGGL(gemm_i8_kernel<EPI_SWIGLU>, grid, blk, 0, st, t, mt); break;
-    default: return hipErrorInvalidValue;
+  const I8Plan p = plan_i8(M, N, K);
+  if (plan_ws_bytes(p, M, N) > ws_bytes) return hipErrorInvalidValue;
+  return run_i8_plan(p, {a, a_scale, w, w_scale, c, M, N, K, epi == EPI_SWIGLU ? N / 2 : N, (int32_t*)ws}, epi, st);
+}
+
+// ------------------------------------------------------------------- grouped
+// Expert e owns rows [off[e], off[e] + cnt[e]) of C and of a_scale, and of A or of
+// the row list into A; mtiles lists the non-empty row tiles (e << 16 | tile).
+// Persistent blocks take items (row tile, column tile), column tile fastest.
+struct I8Groups {
+  const int32_t *off, *cnt, *mtiles, *n_mtiles, *arow;
+};
+
+// Ring tiles.  With gathered rows each XCD takes a contiguous eighth of the items,
+// so the column tiles of an expert's row tile find its rows in that XCD's L2.
+template <int BM, int BN, int STAGES, int EPI>
+__global__ void __launch_bounds__(256)
+    gemm_i8_grouped_kernel(const int8_t* __restrict__ A, const float* __restrict__ a_scale, const int8_t* __restrict__ W,
+                           const float* __restrict__ w_scale, void* __restrict__ C, int ldc, int N, int K2, int nt, I8Groups g) {
+  constexpr int esz = (EPI == EPI_F32 || EPI == EPI_ADD_F32) ? 4 : 2;
+  const int total = g.n_mtiles[0] * nt;
+  const bool by_xcd = g.arow != nullptr;
+  const int chunk = (total + 7) >> 3;
+  const int lo = by_xcd ? (int)(blockIdx.x & 7) * chunk : 0, hi = by_xcd ? min(total, lo + chunk) : total;
+  const int step = by_xcd ? (int)(gridDim.x >> 3) : (int)gridDim.x;
+  for (int it = by_xcd ? lo + (int)(blockIdx.x >> 3) : (int)blockIdx.x; it < hi; it += step) {
+    const int mt = g.mtiles[it / nt], ni = it % nt;
+    const int e = mt >> 16, mi = mt & 0xffff;
+    const int64_t off = g.off[e];
+    // other wavefronts may still read the last LDS stage of the item before
+    __builtin_amdgcn_s_barrier();
+    const I8Op::Extra ex{a_scale + off, w_scale + (int64_t)e * N, K2};
+    dma_gemm_tile<I8Op, BM, BN, 64, 2, 2, STAGES, EPI, false>(
+        (const bf16_t*)A + (g.arow ? 0 : off * K2), K2, (const bf16_t*)W + (int64_t)e * N * K2, K2,
+        (char*)C + off * ldc * esz, ldc, g.cnt[e], N, K2, mi, ni, 0, nullptr, g.arow ? g.arow + off : nullptr, ex);
   }
+}
+
+// 256 x 256 tiles of the alternating groups, items in eighths by XCD.
+template <int EPI>
+__global__ void __launch_bounds__(512, 2)
+    gemm_i8_alt_grouped_kernel(const int8_t* __restrict__ A, const float* __restrict__ a_scale, const int8_t* __restrict__ W,
+                               const float* __restrict__ w_scale, void* __restrict__ C, int ldc, int N, int K2, int nt,
+                               I8Groups g) {
+  constexpr int esz = (EPI == EPI_F32 || EPI == EPI_ADD_F32) ? 4 : 2;
+  constexpr int BM = 256, BN = 256;
+  const int total = g.n_mtiles[0] * nt, chunk = (total + 7) >> 3;
+  const int hi = min(total, ((int)(blockIdx.x & 7) + 1) * chunk);
+  int it = (int)(blockIdx.x & 7) * chunk + (int)(blockIdx.x >> 3);
+  auto next = [&](AltItem& t) {
+    if (it >= hi) return false;
+    const int mt = g.mtiles[it / nt], ni = it % nt;
+    it += (int)(gridDim.x >> 3);
+    const int e = mt >> 16, m0 = (mt & 0xffff) * BM;
+    const int64_t row = (int64_t)g.off[e] + m0;
+    t.a = (const bf16_t*)A + (g.arow ? 0 : row * K2);
+    t.w = (const bf16_t*)W + ((int64_t)e * N + ni * BN) * K2;
+    t.c = (char*)C + (row * ldc + (EPI == EPI_SWIGLU ? ni * BN / 2 : ni * BN)) * esz;
+    t.rows = g.cnt[e] - m0;
+    t.arow = g.arow ? g.arow + row : nullptr;
+    t.a_scale = a_scale + row;
+    t.w_scale = w_scale + (int64_t)e * N + ni * BN;
+    t.cols = N - ni * BN;
+    return true;
+  };
+  alt_gemm_items<I8Op, BM, BN, 2, 4, EPI, false, false>(K2, K2, ldc, K2 / 64, next);
+}
+
+// Row tile of a projection of `pairs` routed rows.  256 (alternating groups) from 97
+// rows per expert on, where K is whole pairs of K tiles and offsets (of gathered
+// rows: from the first one) fit 32 bits, else 128; below, 64.
+static int grouped_i8_rows(int64_t pairs, int E, int N, int K, int64_t gathered_bytes) {
+  if (pairs <= (int64_t)96 * E) return 64;
+  const bool fits = K % 256 == 0 && gathered_bytes < ((int64_t)1 << 32) &&
+                    (int64_t)256 * std::max<int64_t>(K, 2 * (int64_t)N) < ((int64_t)1 << 31);
+  return fits ? 256 : 128;
+}
+
+template <int BM, int BN, int STAGES, int BPC, int EPI>
+static hipError_t grouped_i8_go(const I8Call& c, const I8Groups& g, hipStream_t st) {
+  constexpr int lds = STAGES * (BM + BN) * 64 * 2;
+  auto kern = gemm_i8_grouped_kernel<BM, BN, STAGES, EPI>;
+  static std::atomic<uint64_t> done{0};
+  hipError_t e = allow_lds((const void*)kern, lds, done);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3(kI8Cus * BPC), dim3(256), lds, st, c.a, c.a_scale, c.w, c.w_scale, c.c, c.ldc, c.N, c.K / 2,
+                     (c.N + BN - 1) / BN, g);
+  return hipGetLastError();
+}
+template <int EPI>
+static hipError_t grouped_i8(int rows, const I8Call& c, const I8Groups& g, hipStream_t st) {
+  if (rows == 64) return grouped_i8_go<64, EPI == EPI_SWIGLU ? 64 : 128, EPI == EPI_SWIGLU ? 4 : 3, 2, EPI>(c, g, st);
+  if (rows == 128) return grouped_i8_go<128, 128, 2, 2, EPI>(c, g, st);
+  constexpr int lds = 2 * 512 * 64 * 2 + kAltScaleBytes;
+  auto kern = gemm_i8_alt_grouped_kernel<EPI>;
+  static std::atomic<uint64_t> done{0};
+  hipError_t e = allow_lds((const void*)kern, lds, done);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3(kI8Cus), dim3(512), lds, st, c.a, c.a_scale, c.w, c.w_scale, c.c, c.ldc, c.N, c.K / 2,
+                     (c.N + 255) / 256, g);
   return hipGetLastError();
 }
 
@@ -200,27 +615,41 @@ __global__ void __launch_bounds__(256) combine_i8_kernel(const bf16_t* __restric
   const int64_t r = blockIdx.x;
   for (int c = threadIdx.x * 8; c < d; c += 256 * 8) {
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < k; ++j) {
-      const int p = pos_of[r * k + j];
-      const float wj = weights[r * k + j];
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      if (p >= 0) v = *(const uint4*)(y + (int64_t)p * d + c);
-      const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+    for (int j0 = 0; j0 < k; j0 += 8) {
+      // eight experts' rows are loaded before any is added
+      X8<true> v[8];
+      float wj[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[2 * i] = fmaf(wj, bf16_to_f32((bf16_t)(u[i] & 0xffffu)), s[2 * i]);
-        s[2 * i + 1] = fmaf(wj, bf16_to_f32((bf16_t)(u[i] >> 16)), s[2 * i + 1]);
+      for (int j = 0; j < 8; ++j) {
+        wj[j] = 0.f;
+        v[j].v = (u32x4_t){0u, 0u, 0u, 0u};
+        if (j0 + j < k) {
+          const int p = pos_of[r * k + j0 + j];
+          wj[j] = weights[r * k + j0 + j];
+          if (p >= 0) v[j].load(y, (int64_t)p * d + c);
+        }
       }
-    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) store_i8<EPI>(out, r * d + c + i, s[i]);
+      for (int j = 0; j < 8; ++j)
+        if (j0 + j < k)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s[i] = fmaf(wj[j], v[j].at(i), s[i]);
+    }
+    if constexpr (EPI == EPI_ADD_F32) {
+      f32x4_t* o = (f32x4_t*)((float*)out + r * d + c);
+      o[0] += (f32x4_t){s[0], s[1], s[2], s[3]};
+      o[1] += (f32x4_t){s[4], s[5], s[6], s[7]};
+    } else {
+      *(u32x4_t*)((bf16_t*)out + r * d + c) = (u32x4_t){f32_to_bf16x2(s[0], s[1]), f32_to_bf16x2(s[2], s[3]),
+                                                        f32_to_bf16x2(s[4], s[5]), f32_to_bf16x2(s[6], s[7])};
+    }
   }
 }
 
 // Workspace of the expert layer, in this order, each part 256-byte aligned.
 struct FfnWork {
   int8_t *q, *hq;
-  float *q_scale, *h_scale;
+  float *q_scale, *pos_scale, *h_scale;
   int32_t *counts, *offsets, *mtiles, *n_mtiles, *mtiles_dn, *n_mtiles_dn, *blk, *pos_of, *row_of;
   bf16_t *h, *y;
 };
@@ -235,6 +664,7 @@ static size_t ffn_layout(int64_t rows, int d, int E, int k, int Fe, char* base, 
   FfnWork t;
   t.q = (int8_t*)part((size_t)rows * d);
   t.q_scale = (float*)part((size_t)rows * 4);
+  t.pos_scale = (float*)part(pairs * 4);
   t.counts = (int32_t*)part((size_t)E * 4);
   t.offsets = (int32_t*)part((size_t)E * 4);
   t.mtiles = (int32_t*)part((pairs / kGroupedTileRowsMin + E) * 4);
@@ -266,15 +696,18 @@ hipError_t launch_moe_ffn_i8(const FfnI8Args& a, hipStream_t st) {
   l.topk_id = a.ids; l.n_pairs = n_pairs; l.E = a.E; l.k = a.k;
   l.counts = f.counts; l.offsets = f.offsets;
   l.mtiles = f.mtiles; l.n_mtiles = f.n_mtiles; l.mtiles_dn = f.mtiles_dn; l.n_mtiles_dn = f.n_mtiles_dn;
-  l.tile_rows = l.tile_rows_dn = kGroupedTileRowsMin;
+  l.tile_rows = grouped_i8_rows(n_pairs, a.E, 2 * a.Fe, a.d, (int64_t)a.n_rows * a.d);
+  l.tile_rows_dn = grouped_i8_rows(n_pairs, a.E, a.d, a.Fe, 0);
   l.blk = f.blk; l.pos_of = f.pos_of; l.row_of = f.row_of;
+  l.row_scale = f.q_scale; l.pos_scale = f.pos_scale;
   if ((e = launch_moe_lists(l, st)) != hipSuccess) return e;
-  const I8Groups gu{f.offsets, f.counts, f.mtiles, f.n_mtiles}, dn{f.offsets, f.counts, f.mtiles_dn, f.n_mtiles_dn};
-  const I8Tile t1{f.q, a.w_gu, f.q_scale, a.s_gu, f.h, 0, 2 * a.Fe, a.d, a.Fe, f.row_of};
-  hipLaunchKernelGGL(gemm_i8_grouped_kernel<EPI_SWIGLU>, dim3(1024), dim3(256), 0, st, t1, gu, (2 * a.Fe + 63) / 64);
+  const I8Call gu{f.q, f.pos_scale, a.w_gu, a.s_gu, f.h, 0, 2 * a.Fe, a.d, a.Fe, nullptr};
+  if ((e = grouped_i8<EPI_SWIGLU>(l.tile_rows, gu, {f.offsets, f.counts, f.mtiles, f.n_mtiles, f.row_of}, st)) != hipSuccess)
+    return e;
   if ((e = launch_quantize_rows(f.h, n_pairs, a.Fe, a.Fe, true, f.hq, f.h_scale, st)) != hipSuccess) return e;
-  const I8Tile t2{f.hq, a.w_down, f.h_scale, a.s_down, f.y, 0, a.d, a.Fe, a.d, nullptr};
-  hipLaunchKernelGGL(gemm_i8_grouped_kernel<EPI_BF16>, dim3(1024), dim3(256), 0, st, t2, dn, (a.d + 63) / 64);
+  const I8Call dn{f.hq, f.h_scale, a.w_down, a.s_down, f.y, 0, a.d, a.Fe, a.d, nullptr};
+  if ((e = grouped_i8<EPI_BF16>(l.tile_rows_dn, dn, {f.offsets, f.counts, f.mtiles_dn, f.n_mtiles_dn, nullptr}, st)) != hipSuccess)
+    return e;
   if (a.epi == EPI_ADD_F32)
     hipLaunchKernelGGL(combine_i8_kernel<EPI_ADD_F32>, dim3(a.n_rows), dim3(256), 0, st, f.y, a.d, a.k, f.pos_of,
                        a.weights, a.out);

@@ -195,7 +195,8 @@ __device__ __forceinline__ int moe_lists(const MoeLists& l, int v, int E, int32_
 // its expert's segment (cursor[e], in LDS), pos_of and its inverse row_of.
 __device__ __forceinline__ void moe_place(const int32_t* __restrict__ topk_id, int beg, int end, int E, int k,
                                           int32_t* cursor, int32_t* __restrict__ pos_of,
-                                          int32_t* __restrict__ row_of) {
+                                          int32_t* __restrict__ row_of, const float* __restrict__ row_scale,
+                                          float* __restrict__ pos_scale) {
   for (int i = beg + (int)threadIdx.x; i < end; i += 1024) {
     const int e = topk_id[i];
     if (e < 0 || e >= E) {
@@ -205,6 +206,7 @@ __device__ __forceinline__ void moe_place(const int32_t* __restrict__ topk_id, i
     const int p = atomicAdd(&cursor[e], 1);
     pos_of[i] = p;
     row_of[p] = i / k;
+    if (pos_scale) pos_scale[p] = row_scale[i / k];
   }
 }
 
@@ -212,7 +214,9 @@ __device__ __forceinline__ void moe_place(const int32_t* __restrict__ topk_id, i
 // the n_pairs routed (row, slot) pairs.
 __global__ void __launch_bounds__(1024) moe_offsets_kernel(const int32_t* __restrict__ topk_id, int n_pairs, int E,
                                                            int k, MoeLists lists, int32_t* __restrict__ pos_of,
-                                                           int32_t* __restrict__ row_of) {
+                                                           int32_t* __restrict__ row_of,
+                                                           const float* __restrict__ row_scale,
+                                                           float* __restrict__ pos_scale) {
   __shared__ int32_t hist[1024];
   __shared__ int32_t sh[32];
   const int tid = threadIdx.x;
@@ -226,7 +230,7 @@ __global__ void __launch_bounds__(1024) moe_offsets_kernel(const int32_t* __rest
   const int ex = moe_lists(lists, tid < E ? hist[tid] : 0, E, sh);
   hist[tid] = tid < E ? ex : 0;          // the per-expert cursors
   __syncthreads();
-  moe_place(topk_id, 0, n_pairs, E, k, hist, pos_of, row_of);
+  moe_place(topk_id, 0, n_pairs, E, k, hist, pos_of, row_of, row_scale, pos_scale);
 }
 
 // Large batches (the prefill): the pairs go to kMoeBlocks blocks, which count
@@ -269,12 +273,15 @@ __global__ void __launch_bounds__(1024) moe_scan_kernel(int E, MoeLists lists, i
 }
 __global__ void __launch_bounds__(1024) moe_place_kernel(const int32_t* __restrict__ topk_id, int n_pairs, int E,
                                                          int k, const int32_t* __restrict__ blk,
-                                                         int32_t* __restrict__ pos_of, int32_t* __restrict__ row_of) {
+                                                         int32_t* __restrict__ pos_of, int32_t* __restrict__ row_of,
+                                                         const float* __restrict__ row_scale,
+                                                         float* __restrict__ pos_scale) {
   __shared__ int32_t cursor[1024];
   const int tid = threadIdx.x, b = blockIdx.x;
   cursor[tid] = tid < E ? blk[b * E + tid] : 0;
   __syncthreads();
-  moe_place(topk_id, moe_block_begin(b, n_pairs), moe_block_begin(b + 1, n_pairs), E, k, cursor, pos_of, row_of);
+  moe_place(topk_id, moe_block_begin(b, n_pairs), moe_block_begin(b + 1, n_pairs), E, k, cursor, pos_of, row_of,
+            row_scale, pos_scale);
 }
 
 // x[r] += sum_j w[r][j] * y[pos(r, j)]   (slot order, y in bf16, the sum in
@@ -372,12 +379,12 @@ hipError_t launch_moe_lists(const MoeListArgs& a, hipStream_t st) {
                        a.tile_rows, a.tile_rows_dn};
   if (a.n_pairs <= kMoeOneBlockPairs) {
     hipLaunchKernelGGL(moe_offsets_kernel, dim3(1), dim3(1024), 0, st, a.topk_id, a.n_pairs, a.E, a.k, lists, a.pos_of,
-                       a.row_of);
+                       a.row_of, a.row_scale, a.pos_scale);
   } else {
     hipLaunchKernelGGL(moe_count_kernel, dim3(kMoeBlocks), dim3(1024), 0, st, a.topk_id, a.n_pairs, a.E, a.blk);
     hipLaunchKernelGGL(moe_scan_kernel, dim3(1), dim3(1024), 0, st, a.E, lists, a.blk);
     hipLaunchKernelGGL(moe_place_kernel, dim3(kMoeBlocks), dim3(1024), 0, st, a.topk_id, a.n_pairs, a.E, a.k, a.blk,
-                       a.pos_of, a.row_of);
+                       a.pos_of, a.row_of, a.row_scale, a.pos_scale);
   }
   return hipGetLastError();
 }
@@ -417,7 +424,7 @@ hipError_t launch_moe_ffn(const MoeArgs& a, hipStream_t st, bool* normed) {
 #undef DARTS_TOPK
   const MoeListArgs lists{a.topk_id, a.n_rows * a.k, a.E, a.k, a.counts, a.offsets, a.mtiles, a.n_mtiles, a.mtiles_dn,
                           a.n_mtiles_dn, plan_gu.tile_rows, plan_dn.tile_rows, a.touched_out, a.blk, a.pos_of,
-                          a.row_of};
+                          a.row_of, nullptr, nullptr};
   if ((e = launch_moe_lists(lists, st)) != hipSuccess) return e;
   const int Fe = a.Fe, d = a.d;
   // gate/up: N = 2*Fe, K = d (SwiGLU into h_perm), A rows gathered from xn;

@@ -35,11 +35,11 @@ def _dt(B, t):
     return B.DARTS_BF16 if t.dtype == torch.bfloat16 else B.DARTS_F32
 
 
-def quantize(x, stream=None):
+def quantize(x):
     B = _b()
     q = torch.full((x.shape[0] + 1, x.shape[1]), 99, dtype=torch.int8, device=DEV)
     s = torch.full((x.shape[0] + 1,), 99.0, device=DEV)
-    B.darts_quantize_rows(x, _dt(B, x), q, s, stream=stream)
+    B.darts_quantize_rows(x, _dt(B, x), q, s)
     torch.cuda.synchronize()
     assert bool((q[-1] == 99).all()) and float(s[-1]) == 99.0
     return q[:-1].contiguous(), s[:-1].contiguous()
@@ -113,6 +113,8 @@ def product(a, sa, w, sw, epi, stream=None):
     cols = N // 2 if epi == 3 else N
     out = torch.full((M + 70, cols), 3.0, dtype=torch.float32 if epi in (0, 2) else torch.bfloat16, device=DEV)
     ws = torch.full((B.darts_gemm_i8_workspace_bytes(M, N, K) + 256,), 0x5a, dtype=torch.uint8, device=DEV)
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())       # for what was just filled
     B.darts_gemm_i8(a, sa, w, sw, out, M, N, K, epi, ws[:-256], stream=stream)
     torch.cuda.synchronize()
     assert bool((out[M:] == 3.0).all()) and bool((ws[-256:] == 0x5a).all())
@@ -186,7 +188,6 @@ def test_product_is_the_same_every_time_and_on_any_stream():
     a, sa, w, sw = _operands(45, 4096, 12288)
     one = product(a, sa, w, sw, 0)
     st = torch.cuda.Stream()
-    st.wait_stream(torch.cuda.current_stream())
     assert torch.equal(one, product(a, sa, w, sw, 0, stream=st)) and torch.equal(one, product(a, sa, w, sw, 0))
 
 
@@ -230,6 +231,8 @@ def ffn(x, ids, w, layer, epi=1, stream=None):
     out = torch.full((R + 3, d), 2.0, dtype=torch.bfloat16 if epi == 1 else torch.float32, device=DEV)
     ws = torch.full((B.darts_moe_ffn_i8_workspace_bytes(R, d, E, ids.shape[1], F2 // 2) + 256,), 0xff, dtype=torch.uint8,
                     device=DEV)
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
     B.darts_moe_ffn_i8(x, ids, w, E, F2 // 2, *layer, out, epi, ws[:-256], stream=stream)
     torch.cuda.synchronize()
     assert bool((out[R:] == 2.0).all()) and bool((ws[-256:] == 0xff).all())

@@ -23,6 +23,8 @@ def _call(logits, k, score="softmax", bias=None, n_groups=1, top_groups=1, group
     B = _b()
     ids = torch.full((logits.shape[0] + 1, k), 77, dtype=torch.int32, device=DEV)
     w = torch.full((logits.shape[0] + 1, k), 77.0, device=DEV)
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())       # for what was just filled
     B.darts_moe_route(logits, B.DARTS_BF16 if logits.dtype == torch.bfloat16 else B.DARTS_F32, ids[:-1], w[:-1],
                       score=B.SCORE_SIGMOID if score == "sigmoid" else B.SCORE_SOFTMAX, bias=bias, n_groups=n_groups,
                       top_groups=top_groups, group_best=group_best, renorm=renorm, factor=factor, stream=stream)
@@ -131,7 +133,6 @@ def test_other_stream_and_graph_replays():
     l = _logits(300, 256)
     exp = _call(l, 8, score="sigmoid", n_groups=8, top_groups=4, group_best=2)
     st = torch.cuda.Stream()
-    st.wait_stream(torch.cuda.current_stream())
     got = _call(l, 8, score="sigmoid", n_groups=8, top_groups=4, group_best=2, stream=st)
     assert (got[0] == exp[0]).all() and (got[1] == exp[1]).all()
     ids = torch.zeros(300, 8, dtype=torch.int32, device=DEV)
