@@ -605,8 +605,7 @@ typedef enum { DARTS_SCORE_SOFTMAX = 0, DARTS_SCORE_SIGMOID = 1 } darts_score;
  * largest t are chosen, in that order.  Ties go to the lower id or group.  The
  * weight of a chosen expert is its s (without the bias), divided by the sum of
  * the chosen ones' when renorm != 0 (0 if that sum is 0), times factor.
- * Scores are 64-bit (float32 weights come out); two that agree to 42 bits count
- * as equal.
+ * Scores are 64-bit; the weights are rounded to float32.
  *   d_logits  [n_rows] rows of n_experts (bf16 or f32), ld elements apart
  *   d_bias    NULL or [n_experts] float32
  *   d_ids     [n_rows][top_k] int32 out

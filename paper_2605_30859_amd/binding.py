@@ -145,10 +145,15 @@ def _ptr(t):
 
 
 def _stream(stream):
-    if stream is None:
-        import torch
-        stream = torch.cuda.current_stream()
-    return C.c_void_p(stream.cuda_stream)
+    """The stream's handle; None: torch's current stream of the current device.  (A
+    torch.cuda.current_stream() object costs 2.6 us, a third of a small call.)"""
+    if stream is not None:
+        return stream.cuda_stream
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is None:
+        return torch.cuda.current_stream().cuda_stream
+    return raw(torch.cuda.current_device())
 
 
 def _check(status, ctx=None):

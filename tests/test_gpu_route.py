@@ -111,11 +111,42 @@ def test_ties_go_to_the_lower_id():
             _check(l, 5, score="sigmoid", **kw)
 
 
+@pytest.mark.parametrize("E,k", [(64, 8), (128, 8), (256, 8), (500, 20), (1024, 40)])
+def test_nearly_equal_scores(E, k):
+    """Neighbours a few last digits apart, in the logits and after the bias, beside
+    equal ones: the 64-bit order decides."""
+    g = torch.Generator(device=DEV).manual_seed(E)
+    base = torch.randint(0, 6, (40, E), device=DEV, generator=g).float() * 0.25
+    step = torch.randint(0, 3, (40, E), device=DEV, generator=g).float()
+    l = base + step * torch.tensor([2.0 ** -23, 2.0 ** -20, 2.0 ** -17, 2.0 ** -15], device=DEV).repeat(10)[:, None]
+    l[::2] -= 0.75
+    bias = torch.randint(0, 4, (E,), device=DEV, generator=g).float() * 0.125
+    for score in ("softmax", "sigmoid"):
+        for b in (None, bias, bias + step[0] * 2.0 ** -22):
+            _check(l, k, score=score, bias=b)
+            _check(l, k, score=score, bias=b, n_groups=4, top_groups=2, group_best=2)
+            _check(l.bfloat16(), k, score=score, bias=b)
+        _check(l + 20.0, k, score=score)
+        _check(l * 8.0 - 690.0, k, score=score)
+
+
+@pytest.mark.parametrize("bias", [-1000.0, 3e4])
+def test_large_bias(bias):
+    l = _logits(30, 128)
+    b = torch.full((128,), bias, device=DEV) + torch.arange(128, device=DEV) % 5
+    for score in ("softmax", "sigmoid"):
+        _check(l, 8, score=score, bias=b)
+
+
 def test_strided_rows():
     wide = _logits(50, 384)
     wide[:, 60:] = float("nan")       # columns beside the logits are not read
     _check(wide[:, :60], 4)
     _check(wide.bfloat16()[:, :60], 4)
+    _check(wide[:, 1:61].nan_to_num(0.5), 4)
+    flat = _logits(1, 4000).flatten()                     # rows that begin at any address
+    _check(torch.as_strided(flat, (30, 64), (67, 1), 1), 6)
+    _check(torch.as_strided(flat.bfloat16(), (30, 64), (66, 1), 3), 6)
 
 
 def test_many_rows():
