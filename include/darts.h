@@ -639,7 +639,8 @@ int darts_quantize_rows(const void* d_x, int64_t ldx, int32_t rows, int32_t cols
  * float32 d_c, 3 SwiGLU (W rows and their scales interleaved in groups of 16;
  * d_c [M][N/2] bf16).
  *   d_a [M][K], d_w [N][K] codes, 16-byte aligned; K and N multiples of 16 (N of
- *   32 for SwiGLU), K <= 131072 (so that the sum fits).  d_workspace must hold
+ *   32 for SwiGLU), K <= 131072 (so that the sum fits), and fewer than 2^24 tiles
+ *   of 64 x 64 results.  d_workspace must hold
  *   darts_gemm_i8_workspace_bytes(M, N, K) bytes, 16-byte aligned.         */
 size_t darts_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K);
 int darts_gemm_i8(const int8_t* d_a, const float* d_a_scale, const int8_t* d_w, const float* d_w_scale,

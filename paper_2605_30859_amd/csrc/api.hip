@@ -1404,12 +1404,12 @@ int darts_quantize_rows(const void* d_x, int64_t ldx, int32_t rows, int32_t cols
   if (dtype != DARTS_F32 && dtype != DARTS_BF16) return DARTS_EINVAL;
   if (rows == 0) return DARTS_OK;
   if (!d_x || !d_q || !d_scale) return DARTS_EINVAL;
-  hipError_t e = launch_quantize_rows(d_x, rows, cols, ldx, dtype == DARTS_BF16, d_q, d_scale, (hipStream_t)stream);
+  hipError_t e = launch_quantize_rows(d_x, rows, cols, ldx, dtype == DARTS_BF16, d_q, cols, d_scale, (hipStream_t)stream);
   return e == hipSuccess ? DARTS_OK : DARTS_EHIP;
 }
 
 constexpr int kI8MaxK = 131072;   // 127 * 127 * 131072 < 2^31
-constexpr int64_t kI8MaxPairs = (int64_t)65535 * kGroupedTileRowsMin;   // an expert's row tiles fit 16 bits
+constexpr int64_t kI8MaxPairs = (int64_t)65535 * 64;   // an expert's row tiles fit 16 bits
 
 size_t darts_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K) {
   if (M < 1 || N < 1 || K < 1) return 0;
@@ -1421,6 +1421,7 @@ int darts_gemm_i8(const int8_t* d_a, const float* d_a_scale, const int8_t* d_w, 
                   size_t workspace_bytes, void* stream) {
   if (M < 0 || N < 1 || K < 1 || N % 16 || K % 16 || K > kI8MaxK) return DARTS_EINVAL;
   if (epilogue < 0 || epilogue > 3 || (epilogue == 3 && N % 32)) return DARTS_EINVAL;
+  if (((int64_t)M + 63) / 64 * (((int64_t)N + 63) / 64) >= (1 << 24)) return DARTS_EINVAL;   // too many tiles for a launch
   if (M == 0) return DARTS_OK;
   if (!d_a || !d_a_scale || !d_w || !d_w_scale || !d_c) return DARTS_EINVAL;
   if (!aligned16(d_a) || !aligned16(d_w) || !aligned16(d_workspace)) return DARTS_EINVAL;

@@ -390,10 +390,12 @@ struct AltItem {
 // strip-packed (ldw = K).  An item's row list is read during the last K tiles of
 // the item before it, and its first loads are issued before that item's results
 // are stored, so neither latency is waited for (EPI_ADD_F32 reads the results'
-// old values behind those loads, and waits for them).
+// old values behind those loads, and waits for them).  TAIL: W's rows hold w_units of
+// K, less than nk tiles; A's are zero from there on, and W's loads past the end read
+// codes before it instead.
 constexpr int kAltScaleBytes = 2 * 512 * 4;   // codes: dynamic LDS beyond the tiles
-template <typename Op, int BM, int BN, int WGM, int WGN, int EPI, bool SPLIT, bool PW, typename Next>
-__device__ __forceinline__ void alt_gemm_items(int lda, int ldw, int ldc, int nk, Next next) {
+template <typename Op, int BM, int BN, int WGM, int WGN, int EPI, bool SPLIT, bool PW, int WAUX = 0, bool TAIL = false, typename Next>
+__device__ __forceinline__ void alt_gemm_items(int lda, int ldw, int ldc, int nk, Next next, [[maybe_unused]] int w_units = 0) {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass knows no buffer resources
   constexpr int KB = 64, NW = 8;
   static_assert(WGM * WGN == NW, "8 wavefronts");
@@ -434,7 +436,7 @@ __device__ __forceinline__ void alt_gemm_items(int lda, int ldw, int ldc, int nk
   // results, 0.43 ms of its 1.03 ms.)  Otherwise rows are in order.
   constexpr bool kPair = kEsz == 2 && TN % 2 == 0;
   const int wlane = kPair ? 8 * (lrow >> 2) + (lrow & 3) : lrow;   // row in a strip of 16, but for a uniform part
-  const int woff = PW ? ((gchunk & 3) * 16 + wlane) * 16 + (gchunk >> 2) * 1024 : (wlane * ldw + gchunk * 8) * 2;
+  int woff = PW ? ((gchunk & 3) * 16 + wlane) * 16 + (gchunk >> 2) * 1024 : (wlane * ldw + gchunk * 8) * 2;
   auto row_ids = [&](const AltItem& t, int (&row)[2][LA]) {
     int row0 = lrow;
     asm volatile("" : "+v"(row0));                    // recomputed here, not kept over the K loop
@@ -461,9 +463,22 @@ __device__ __forceinline__ void alt_gemm_items(int lda, int ldw, int ldc, int nk
                                                kt * (KB * 2), 0, 0);
   };
   [[maybe_unused]] int w_rows = 0;
+  [[maybe_unused]] const int w_full = w_units / KB, w_rest = w_units % KB;   // whole K tiles of W, units of the next
+  // woff for whole K tiles, and for the one that W ends in
+  [[maybe_unused]] auto w_offset = [&](bool end) {
+    int l = lane;
+    asm volatile("" : "+v"(l));                       // computed where it changes, not kept
+    const int r = l >> 3, c = (l & 7) ^ r;
+    return ((kPair ? 8 * (r >> 2) + (r & 3) : r) * ldw + (end && c * 8 >= w_rest ? 0 : c * 8)) * 2;
+  };
   if constexpr (Op::kI8) w_rows = cur.cols;
   auto issue_b = [&](int kt, int stage, int h) {
     bf16_t* s = smem + 4 * HA + (2 * h + stage) * HB + wave * 8 * KB;
+    if constexpr (TAIL)
+      if (kt >= w_full) {
+        kt = w_rest ? w_full : w_full - 1;
+        if (w_rest) woff = w_offset(true);
+      }
 #pragma unroll
     for (int j = 0; j < LB; ++j) {
       if (j == LB1 && !first) break;
@@ -473,7 +488,7 @@ __device__ __forceinline__ void alt_gemm_items(int lda, int ldw, int ldc, int nk
       int row = (kSwiglu ? strip * 2 + h : strip / TN * 2 * TN + h * TN + strip % TN) * 16;
       if constexpr (Op::kI8) row = min(row, w_rows - 16);   // a strip past W's last one repeats it
       const int off = PW ? row * 2 * ldw + sub * 16 + kt * (KB * 32) : (row + sub) * 2 * ldw + kt * (KB * 2);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(wres, (lds_void_t*)(s + NW * j * 8 * KB), 16, woff, off, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(wres, (lds_void_t*)(s + NW * j * 8 * KB), 16, woff, off, 0, WAUX);
     }
   };
 
@@ -578,6 +593,8 @@ __device__ __forceinline__ void alt_gemm_items(int lda, int ldw, int ldc, int nk
   [[maybe_unused]] int turn = 0;
   // the first loads of cur, whose rows are in arow
   auto start = [&]() {
+    if constexpr (TAIL)
+      if (w_rest) woff = w_offset(false);
     if constexpr (kScales) {
       int t = lane + 64 * (wave & 3);
       asm volatile("" : "+v"(t));                     // recomputed here, not kept over the K loop

@@ -65,13 +65,14 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
   return v;
 }
 
-// WPR wavefronts per row, blocks of four.  VEC: rows of whole 16-byte pieces; the
-// first kQuantKeep pieces of a lane stay in registers between the two passes, so
+// WPR wavefronts per row, blocks of four.  VEC: rows of whole 16-byte pieces, codes
+// ldq apart with zeros between them (else ldq is cols); the first kQuantKeep pieces of a lane stay in registers between the two passes, so
 // rows of up to 64 * WPR * 32 elements are read once.
 constexpr int kQuantKeep = 4;
 template <bool BF16, bool VEC, int WPR>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const void* __restrict__ x, int64_t rows, int cols, int64_t ldx,
-                                                            int8_t* __restrict__ q, float* __restrict__ scale) {
+                                                            int8_t* __restrict__ q, int64_t ldq,
+                                                            float* __restrict__ scale) {
   __shared__ uint32_t red[4];
   constexpr int T = 64 * WPR;                          // threads of a row
   const int64_t r = (int64_t)blockIdx.x * (4 / WPR) + threadIdx.x / T;
@@ -115,7 +116,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const void* __restri
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[h] |= ((uint32_t)code_of(v.at(4 * h + e), up) & 0xffu) << (8 * e);
     }
-    *(uint2*)(q + r * cols + c * 8) = make_uint2(w[0], w[1]);
+    *(uint2*)(q + r * ldq + c * 8) = make_uint2(w[0], w[1]);
   };
   if constexpr (VEC) {
 #pragma unroll
@@ -126,13 +127,15 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const void* __restri
       v.load(x, r * ldx + c * 8);
       store(v, c);
     }
+    for (int c = n8 + t; c < ldq / 8; c += T) *(uint2*)(q + r * ldq + c * 8) = make_uint2(0u, 0u);
   } else {
-    for (int c = t; c < cols; c += T) q[r * cols + c] = (int8_t)code_of(load_x<BF16>(x, r * ldx + c), up);
+    for (int c = t; c < cols; c += T) q[r * ldq + c] = (int8_t)code_of(load_x<BF16>(x, r * ldx + c), up);
   }
 }
 
 template <bool BF16, bool VEC>
-static hipError_t quantize_go(const void* x, int64_t rows, int cols, int64_t ldx, int8_t* q, float* scale, hipStream_t st) {
+static hipError_t quantize_go(const void* x, int64_t rows, int cols, int64_t ldx, int8_t* q, int64_t ldq, float* scale,
+                              hipStream_t st) {
   // a wavefront per row where it holds the row, and there are rows for every CU
   const int wpr = cols <= 64 * 8 * kQuantKeep && rows >= 2048 ? 1 : 4;
   const int64_t most = (int64_t)(1 << 22) * (4 / wpr);       // rows per launch
@@ -141,20 +144,24 @@ static hipError_t quantize_go(const void* x, int64_t rows, int cols, int64_t ldx
     const dim3 grid((unsigned)((n * wpr + 3) / 4));
     const char* xr = (const char*)x + r * ldx * (BF16 ? 2 : 4);
     if (wpr == 1)
-      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 1>), grid, dim3(256), 0, st, xr, n, cols, ldx, q + r * cols, scale + r);
+      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 1>), grid, dim3(256), 0, st, xr, n, cols, ldx, q + r * ldq,
+                         ldq, scale + r);
     else
-      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 4>), grid, dim3(256), 0, st, xr, n, cols, ldx, q + r * cols, scale + r);
+      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 4>), grid, dim3(256), 0, st, xr, n, cols, ldx, q + r * ldq,
+                         ldq, scale + r);
   }
   return hipGetLastError();
 }
 
-hipError_t launch_quantize_rows(const void* x, int64_t rows, int cols, int64_t ldx, bool bf16, int8_t* q, float* scale,
-                                hipStream_t st) {
-  const bool vec = cols % 8 == 0 && ((uintptr_t)x & 15) == 0 && ((uintptr_t)q & 7) == 0 && ldx * (bf16 ? 2 : 4) % 16 == 0;
-  if (bf16) return vec ? quantize_go<true, true>(x, rows, cols, ldx, q, scale, st)
-                       : quantize_go<true, false>(x, rows, cols, ldx, q, scale, st);
-  return vec ? quantize_go<false, true>(x, rows, cols, ldx, q, scale, st)
-             : quantize_go<false, false>(x, rows, cols, ldx, q, scale, st);
+hipError_t launch_quantize_rows(const void* x, int64_t rows, int cols, int64_t ldx, bool bf16, int8_t* q, int64_t ldq,
+                                float* scale, hipStream_t st) {
+  const bool vec = cols % 8 == 0 && ldq % 8 == 0 && ((uintptr_t)x & 15) == 0 && ((uintptr_t)q & 7) == 0 &&
+                   ldx * (bf16 ? 2 : 4) % 16 == 0;
+  if (!vec && ldq != cols) return hipErrorInvalidValue;
+  if (bf16) return vec ? quantize_go<true, true>(x, rows, cols, ldx, q, ldq, scale, st)
+                       : quantize_go<true, false>(x, rows, cols, ldx, q, ldq, scale, st);
+  return vec ? quantize_go<false, true>(x, rows, cols, ldx, q, ldq, scale, st)
+             : quantize_go<false, false>(x, rows, cols, ldx, q, ldq, scale, st);
 }
 
 // ------------------------------------------------------------------ products
@@ -240,7 +247,7 @@ __global__ void __launch_bounds__(512) gemm_i8_skinny_kernel(const int8_t* __res
   }
 }
 
-template <int BM, int BN, int WGM, int WGN, int STAGES, int EPI, bool SPLIT, int WAUX>
+template <int BM, int BN, int WGM, int WGN, int STAGES, int EPI, bool SPLIT>
 __global__ void __launch_bounds__(64 * WGM * WGN)
     gemm_i8_ring_kernel(const int8_t* __restrict__ A, const float* __restrict__ a_scale, const int8_t* __restrict__ W,
                         const float* __restrict__ w_scale, void* __restrict__ C, int ldc, int M, int N, int K2, int k_chunk,
@@ -248,16 +255,16 @@ __global__ void __launch_bounds__(64 * WGM * WGN)
   const int b = xcd_block();
   const int mi = b % mt, ni = (b / mt) % nt, z = b / (mt * nt);
   const I8Op::Extra ex{a_scale, w_scale, min(k_chunk, K2 - z * k_chunk)};
-  dma_gemm_tile<I8Op, BM, BN, 64, WGM, WGN, STAGES, EPI, SPLIT, false, WAUX>(
+  dma_gemm_tile<I8Op, BM, BN, 64, WGM, WGN, STAGES, EPI, SPLIT>(
       (const bf16_t*)A, K2, (const bf16_t*)W, K2, C, ldc, M, N, k_chunk, mi, ni, z, (float*)ws, nullptr, ex);
 }
 
 // One persistent block per CU, each XCD a contiguous eighth of the tiles.
-template <int BM, int BN, int WGM, int WGN, int EPI, bool SPLIT>
-__global__ void __launch_bounds__(512, 2)
-    gemm_i8_alt_kernel(const int8_t* __restrict__ A, const float* __restrict__ a_scale, const int8_t* __restrict__ W,
-                       const float* __restrict__ w_scale, void* __restrict__ C, int ldc, int M, int N, int K2, int k_chunk,
-                       int mt, int nt, int n_split, int32_t* __restrict__ ws) {
+template <int BM, int BN, int WGM, int WGN, int BPC, int EPI, bool SPLIT, bool TAIL>
+__global__ void __launch_bounds__(512, 2 * BPC)
+    gemm_i8_alt_kernel(const int8_t* __restrict__ A, int lda2, const float* __restrict__ a_scale,
+                       const int8_t* __restrict__ W, const float* __restrict__ w_scale, void* __restrict__ C, int ldc, int M,
+                       int N, int K2, int k_chunk, int mt, int nt, int n_split, int32_t* __restrict__ ws) {
   constexpr int esz = (SPLIT || EPI == EPI_F32 || EPI == EPI_ADD_F32) ? 4 : 2;
   const int total = mt * nt * n_split, chunk = (total + 7) >> 3;
   const int hi = min(total, ((int)(blockIdx.x & 7) + 1) * chunk);
@@ -268,7 +275,7 @@ __global__ void __launch_bounds__(512, 2)
     int mi, ni;
     panel_order(it - z * mt * nt, mt, nt, mi, ni);
     it += (int)(gridDim.x >> 3);
-    t.a = (const bf16_t*)A + (int64_t)mi * BM * K2 + z * k_chunk;
+    t.a = (const bf16_t*)A + (int64_t)mi * BM * lda2 + z * k_chunk;
     t.w = (const bf16_t*)W + (int64_t)ni * BN * K2 + z * k_chunk;
     const int64_t out = (int64_t)mi * BM * ldc + (EPI == EPI_SWIGLU && !SPLIT ? ni * BN / 2 : ni * BN);
     t.c = SPLIT ? (char*)(ws + (int64_t)z * M * N + out) : (char*)C + out * esz;
@@ -279,7 +286,7 @@ __global__ void __launch_bounds__(512, 2)
     t.cols = N - ni * BN;
     return true;
   };
-  alt_gemm_items<I8Op, BM, BN, WGM, WGN, EPI, SPLIT, false>(K2, K2, ldc, k_chunk / 64, next);
+  alt_gemm_items<I8Op, BM, BN, WGM, WGN, EPI, SPLIT, false, 0, TAIL>(lda2, K2, ldc, k_chunk / 64, next, K2);
 }
 
 // Partial sums of S splits, scales and epilogue; four columns per thread.
@@ -319,24 +326,27 @@ struct I8Plan {
   int mt, nt;        // tiles
   int S;             // K splits (skinny: wavefronts per strip)
   int k_chunk;       // units per split
+  bool pad;          // A's rows are copied to ones of whole pairs of K tiles first
 };
 // The tiles, and a model of their times: a block's time is fixed + per_k * (K tiles
 // of 128 codes), in us, with one block per CU; with two on a CU, gain is the CU's
-// speed against one block's.  Fitted to 300 sizes (16 shapes, 16 to 16384 rows,
-// weights from memory): the plans that it gives take 1.4% longer on average than
-// the fastest measured one.
+// speed against one block's.  Fitted to 330 sizes (16 shapes, 16 to 16384 rows,
+// weights from memory): the plans that it gives take 1.1% longer on average than
+// the fastest measured one, also against ring tiles of 64 x 128 and 128 x 128,
+// which no plan needs.
 struct I8Tiles {
   int bm, bn, occ;
   bool alt;
   double fixed, per_k, gain;
 };
 static constexpr I8Tiles kI8Tiles[] = {
-    {64, 64, 2, false, 1.21, 0.320, 1.35},  {64, 128, 2, false, 2.11, 0.493, 1.39}, {128, 128, 2, false, 2.82, 0.897, 1.68},
-    {256, 128, 1, true, 2.63, 0.773, 1.0},  {256, 192, 1, true, 3.37, 1.046, 1.0},  {256, 256, 1, true, 4.02, 1.233, 1.0}};
+    {64, 64, 2, false, 1.26, 0.321, 1.37}, {128, 128, 2, true, 1.95, 0.558, 1.19}, {128, 256, 1, true, 2.98, 0.843, 1.0},
+    {256, 128, 1, true, 2.52, 0.787, 1.0}, {256, 192, 1, true, 3.24, 1.077, 1.0},  {256, 256, 1, true, 3.95, 1.270, 1.0}};
 constexpr int kI8Kinds = sizeof(kI8Tiles) / sizeof(kI8Tiles[0]);
 constexpr int kI8Cus = 256;
-constexpr double kI8LaunchUs = 3.25, kI8ReduceUs = 2.2;      // of the launch, of the reduce kernel
-constexpr double kI8ReadMBs = 4.94e6, kI8SplitMBs = 5.7e6;   // bytes per us: operands and results, partial sums
+// us: of a launch, of the reduce kernel, of the kernel that pads rows
+constexpr double kI8LaunchUs = 3.17, kI8ReduceUs = 2.2, kI8PadUs = 3.0;
+constexpr double kI8ReadMBs = 5.01e6, kI8SplitMBs = 5.46e6;   // bytes per us: operands and results, partial sums
 
 static bool set_i8_plan(I8Plan& p, int kind, int S, int M, int N, int K) {
   const int K2 = K / 2;
@@ -344,19 +354,23 @@ static bool set_i8_plan(I8Plan& p, int kind, int S, int M, int N, int K) {
   p.S = S;
   p.mt = p.nt = 0;
   p.k_chunk = K2;
+  p.pad = false;
   if (kind < 0) return M <= 32 && (S == 4 || S == 8);
   const I8Tiles& t = kI8Tiles[kind];
   p.mt = (M + t.bm - 1) / t.bm;
   p.nt = (N + t.bn - 1) / t.bn;
   if (t.alt) {
-    // whole pairs of K tiles; 32-bit byte offsets inside a tile
-    if (K2 % (128 * S) || (int64_t)256 * std::max<int64_t>(K, 4 * (int64_t)N) >= ((int64_t)1 << 31)) return false;
-    p.k_chunk = K2 / S;
+    // whole pairs of K tiles (one split: A's rows are padded to them); 32-bit byte
+    // offsets inside a tile
+    if ((int64_t)256 * std::max<int64_t>(K + 256, 4 * (int64_t)N) >= ((int64_t)1 << 31)) return false;
+    if (S > 1 && K2 % (128 * S)) return false;
+    p.pad = K2 % 128 != 0;
+    p.k_chunk = (K2 + 127) / 128 * 128 / S;
   } else {
     p.k_chunk = (K2 + 64 * S - 1) / (64 * S) * 64;
     if ((int64_t)p.k_chunk * (S - 1) >= K2) return false;      // a split without work
   }
-  return (int64_t)p.mt * p.nt * S <= INT32_MAX / 512;
+  return (int64_t)p.mt * p.nt * S < (1 << 24);
 }
 
 static double i8_estimate(const I8Plan& p, int M, int N, int K) {
@@ -365,6 +379,7 @@ static double i8_estimate(const I8Plan& p, int M, int N, int K) {
   double us = blocks <= kI8Cus ? tile : std::ceil(blocks / (t.occ * kI8Cus)) * t.occ * tile / t.gain;
   us = std::max(us, ((double)N * K + (double)M * K + 2.0 * M * N) / kI8ReadMBs) + kI8LaunchUs;
   if (p.S > 1) us += kI8ReduceUs + 8.0 * p.S * M * N / kI8SplitMBs;
+  if (p.pad) us += kI8PadUs;
   return us;
 }
 
@@ -380,9 +395,10 @@ static bool skinny_i8_plan(I8Plan& p, int M, int N, int K) {
   return set_i8_plan(p, -1, N >= 16 * 384 && K <= 4096 ? 4 : 8, M, N, K);
 }
 
-static I8Plan plan_i8(int M, int N, int K) {
-  I8Plan best, p;
-  if (skinny_i8_plan(best, M, N, K)) return best;
+// False if the results are too many for any (2^36 elements).
+static bool plan_i8(I8Plan& best, int M, int N, int K) {
+  if (skinny_i8_plan(best, M, N, K)) return true;
+  I8Plan p;
   double least = 1e300;
   for (int kind = 0; kind < kI8Kinds; ++kind)
     for (int S = 1; S <= 8; S *= 2) {
@@ -393,11 +409,30 @@ static I8Plan plan_i8(int M, int N, int K) {
         best = p;
       }
     }
-  return best;
+  return least < 1e300;
 }
 
-static size_t plan_ws_bytes(const I8Plan& p, int M, int N) { return p.kind >= 0 && p.S > 1 ? (size_t)p.S * M * N * 4 : 0; }
-size_t gemm_i8_workspace_bytes(int M, int N, int K) { return plan_ws_bytes(plan_i8(M, N, K), M, N); }
+static size_t plan_ws_bytes(const I8Plan& p, int M, int N) {
+  if (p.kind < 0) return 0;
+  return p.S > 1 ? (size_t)p.S * M * N * 4 : p.pad ? (size_t)M * p.k_chunk * 2 : 0;
+}
+size_t gemm_i8_workspace_bytes(int M, int N, int K) {
+  I8Plan p;
+  return plan_i8(p, M, N, K) ? plan_ws_bytes(p, M, N) : 0;
+}
+
+// Rows of K codes to rows of ldo, with zeros behind them; 16 bytes per thread.
+__global__ void __launch_bounds__(256) pad_rows_kernel(const int8_t* __restrict__ a, int64_t rows, int K, int ldo,
+                                                       int8_t* __restrict__ out) {
+  const int per = ldo / 16;
+  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < rows * per; t += (int64_t)gridDim.x * 256) {
+    const int64_t r = t / per;
+    const int c = (int)(t % per) * 16;
+    u32x4_t v = {0u, 0u, 0u, 0u};
+    if (c < K) v = *(const u32x4_t*)(a + r * K + c);
+    *(u32x4_t*)(out + r * ldo + c) = v;
+  }
+}
 
 // Dynamic LDS beyond 64 KB is allowed once per kernel and device.
 static hipError_t allow_lds(const void* kern, int bytes, std::atomic<uint64_t>& done) {
@@ -417,7 +452,7 @@ struct I8Call {
   const int8_t* w;
   const float* w_scale;
   void* c;
-  int M, N, K, ldc;
+  int M, N, K, lda, ldc;
   int32_t* ws;
 };
 
@@ -437,7 +472,7 @@ static void skinny_i8(int wk, const I8Call& c, hipStream_t st) {
 template <int EPI, int BM, int BN, int WGM, int WGN, int ST, bool SPLIT>
 static hipError_t ring_i8_go(const I8Plan& p, const I8Call& c, hipStream_t st) {
   constexpr int lds = ST * (BM + BN) * 64 * 2;
-  auto kern = gemm_i8_ring_kernel<BM, BN, WGM, WGN, ST, EPI, SPLIT, 0>;
+  auto kern = gemm_i8_ring_kernel<BM, BN, WGM, WGN, ST, EPI, SPLIT>;
   static std::atomic<uint64_t> done{0};
   hipError_t e = allow_lds((const void*)kern, lds, done);
   if (e != hipSuccess) return e;
@@ -446,28 +481,34 @@ static hipError_t ring_i8_go(const I8Plan& p, const I8Call& c, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <int EPI, int BM, int BN, int WGM, int WGN, bool SPLIT>
-static hipError_t alt_i8_go(const I8Plan& p, const I8Call& c, hipStream_t st) {
+template <int EPI, int BM, int BN, int WGM, int WGN, int BPC, bool SPLIT, bool TAIL>
+static hipError_t alt_i8_as(const I8Plan& p, const I8Call& c, hipStream_t st) {
   constexpr int lds = 2 * (BM + BN) * 64 * 2 + (SPLIT ? 0 : kAltScaleBytes);
-  auto kern = gemm_i8_alt_kernel<BM, BN, WGM, WGN, EPI, SPLIT>;
+  auto kern = gemm_i8_alt_kernel<BM, BN, WGM, WGN, BPC, EPI, SPLIT, TAIL>;
   static std::atomic<uint64_t> done{0};
   hipError_t e = allow_lds((const void*)kern, lds, done);
   if (e != hipSuccess) return e;
-  const int blocks = std::min((p.mt * p.nt * p.S + 7) / 8 * 8, kI8Cus);
-  hipLaunchKernelGGL(kern, dim3(blocks), dim3(512), lds, st, c.a, c.a_scale, c.w, c.w_scale, c.c, SPLIT ? c.N : c.ldc, c.M,
-                     c.N, c.K / 2, p.k_chunk, p.mt, p.nt, p.S, c.ws);
+  const int blocks = std::min((p.mt * p.nt * p.S + 7) / 8 * 8, kI8Cus * BPC);
+  hipLaunchKernelGGL(kern, dim3(blocks), dim3(512), lds, st, c.a, c.lda / 2, c.a_scale, c.w, c.w_scale, c.c,
+                     SPLIT ? c.N : c.ldc, c.M, c.N, c.K / 2, p.k_chunk, p.mt, p.nt, p.S, c.ws);
   return hipGetLastError();
+}
+template <int EPI, int BM, int BN, int WGM, int WGN, int BPC, bool SPLIT>
+static hipError_t alt_i8_go(const I8Plan& p, const I8Call& c, hipStream_t st) {
+  if constexpr (!SPLIT)
+    if (p.pad) return alt_i8_as<EPI, BM, BN, WGM, WGN, BPC, SPLIT, true>(p, c, st);
+  return alt_i8_as<EPI, BM, BN, WGM, WGN, BPC, SPLIT, false>(p, c, st);
 }
 
 template <int EPI, bool SPLIT>
 static hipError_t tiles_i8_go(const I8Plan& p, const I8Call& c, hipStream_t st) {
   switch (p.kind) {
     case 0: return ring_i8_go<EPI, 64, 64, 2, 2, 4, SPLIT>(p, c, st);
-    case 1: return ring_i8_go<EPI, 64, 128, 2, 2, 3, SPLIT>(p, c, st);
-    case 2: return ring_i8_go<EPI, 128, 128, 2, 2, 2, SPLIT>(p, c, st);
-    case 3: return alt_i8_go<EPI, 256, 128, 4, 2, SPLIT>(p, c, st);
-    case 4: return alt_i8_go<EPI, 256, 192, 4, 2, SPLIT>(p, c, st);
-    default: return alt_i8_go<EPI, 256, 256, 2, 4, SPLIT>(p, c, st);
+    case 1: return alt_i8_go<EPI, 128, 128, 2, 4, 2, SPLIT>(p, c, st);
+    case 2: return alt_i8_go<EPI, 128, 256, 2, 4, 1, SPLIT>(p, c, st);
+    case 3: return alt_i8_go<EPI, 256, 128, 4, 2, 1, SPLIT>(p, c, st);
+    case 4: return alt_i8_go<EPI, 256, 192, 4, 2, 1, SPLIT>(p, c, st);
+    default: return alt_i8_go<EPI, 256, 256, 2, 4, 1, SPLIT>(p, c, st);
   }
 }
 
@@ -477,6 +518,15 @@ static hipError_t gemm_i8_go(const I8Plan& p, const I8Call& c, hipStream_t st) {
     if (c.M <= 16) skinny_i8<EPI, 1>(p.S, c, st);
     else skinny_i8<EPI, 2>(p.S, c, st);
     return hipGetLastError();
+  }
+  if (p.pad) {
+    I8Call padded = c;
+    padded.a = (const int8_t*)c.ws;
+    padded.lda = 2 * p.k_chunk;
+    const int64_t n = (int64_t)c.M * padded.lda / 16;
+    hipLaunchKernelGGL(pad_rows_kernel, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 4096)), dim3(256), 0, st, c.a,
+                       (int64_t)c.M, c.K, padded.lda, (int8_t*)c.ws);
+    return tiles_i8_go<EPI, false>(p, padded, st);
   }
   if (p.S == 1) return tiles_i8_go<EPI, false>(p, c, st);
   // partial sums do not depend on the epilogue
@@ -501,107 +551,94 @@ static hipError_t run_i8_plan(const I8Plan& p, const I8Call& c, int epi, hipStre
 hipError_t launch_gemm_i8(const int8_t* a, const float* a_scale, const int8_t* w, const float* w_scale, void* c, int M,
                           int N, int K, int epi, void* ws, size_t ws_bytes, hipStream_t st) {
   if (M <= 0) return hipSuccess;
-  const I8Plan p = plan_i8(M, N, K);
-  if (plan_ws_bytes(p, M, N) > ws_bytes) return hipErrorInvalidValue;
-  return run_i8_plan(p, {a, a_scale, w, w_scale, c, M, N, K, epi == EPI_SWIGLU ? N / 2 : N, (int32_t*)ws}, epi, st);
+  I8Plan p;
+  if (!plan_i8(p, M, N, K) || plan_ws_bytes(p, M, N) > ws_bytes) return hipErrorInvalidValue;
+  return run_i8_plan(p, {a, a_scale, w, w_scale, c, M, N, K, K, epi == EPI_SWIGLU ? N / 2 : N, (int32_t*)ws}, epi, st);
 }
 
 // ------------------------------------------------------------------- grouped
 // Expert e owns rows [off[e], off[e] + cnt[e]) of C and of a_scale, and of A or of
 // the row list into A; mtiles lists the non-empty row tiles (e << 16 | tile).
-// Persistent blocks take items (row tile, column tile), column tile fastest.
+// Persistent blocks take items (row tile, column tile), column tile fastest; each
+// XCD takes a contiguous eighth of them, so the column tiles of an expert's row
+// tile find its rows in that XCD's L2.
 struct I8Groups {
   const int32_t *off, *cnt, *mtiles, *n_mtiles, *arow;
 };
+#define DARTS_GROUP_PARAMS                                                                                       \
+  const int32_t *__restrict__ g_off, const int32_t *__restrict__ g_cnt, const int32_t *__restrict__ mtiles,      \
+      const int32_t *__restrict__ n_mtiles, const int32_t *__restrict__ arow
+#define DARTS_GROUP_ARGS(g) g.off, g.cnt, g.mtiles, g.n_mtiles, g.arow
 
-// Ring tiles.  With gathered rows each XCD takes a contiguous eighth of the items,
-// so the column tiles of an expert's row tile find its rows in that XCD's L2.
-template <int BM, int BN, int STAGES, int EPI>
-__global__ void __launch_bounds__(256)
-    gemm_i8_grouped_kernel(const int8_t* __restrict__ A, const float* __restrict__ a_scale, const int8_t* __restrict__ W,
-                           const float* __restrict__ w_scale, void* __restrict__ C, int ldc, int N, int K2, int nt, I8Groups g) {
-  constexpr int esz = (EPI == EPI_F32 || EPI == EPI_ADD_F32) ? 4 : 2;
-  const int total = g.n_mtiles[0] * nt;
-  const bool by_xcd = g.arow != nullptr;
-  const int chunk = (total + 7) >> 3;
-  const int lo = by_xcd ? (int)(blockIdx.x & 7) * chunk : 0, hi = by_xcd ? min(total, lo + chunk) : total;
-  const int step = by_xcd ? (int)(gridDim.x >> 3) : (int)gridDim.x;
-  for (int it = by_xcd ? lo + (int)(blockIdx.x >> 3) : (int)blockIdx.x; it < hi; it += step) {
-    const int mt = g.mtiles[it / nt], ni = it % nt;
-    const int e = mt >> 16, mi = mt & 0xffff;
-    const int64_t off = g.off[e];
-    // other wavefronts may still read the last LDS stage of the item before
-    __builtin_amdgcn_s_barrier();
-    const I8Op::Extra ex{a_scale + off, w_scale + (int64_t)e * N, K2};
-    dma_gemm_tile<I8Op, BM, BN, 64, 2, 2, STAGES, EPI, false>(
-        (const bf16_t*)A + (g.arow ? 0 : off * K2), K2, (const bf16_t*)W + (int64_t)e * N * K2, K2,
-        (char*)C + off * ldc * esz, ldc, g.cnt[e], N, K2, mi, ni, 0, nullptr, g.arow ? g.arow + off : nullptr, ex);
-  }
-}
-
-// 256 x 256 tiles of the alternating groups, items in eighths by XCD.
-template <int EPI>
-__global__ void __launch_bounds__(512, 2)
+// Tiles of the alternating groups: 128 rows while the weights are streamed (decode
+// batches; non-temporal, each tile of them is read once), 256 rows above.  A's rows
+// are lda2 units apart, zero from K on up to whole pairs of K tiles.
+template <int BM, int BN, int BPC, int EPI, int WAUX, bool TAIL>
+__global__ void __launch_bounds__(512, 2 * BPC)
     gemm_i8_alt_grouped_kernel(const int8_t* __restrict__ A, const float* __restrict__ a_scale, const int8_t* __restrict__ W,
-                               const float* __restrict__ w_scale, void* __restrict__ C, int ldc, int N, int K2, int nt,
-                               I8Groups g) {
+                               const float* __restrict__ w_scale, void* __restrict__ C, int ldc, int N, int K2, int lda2,
+                               int nt, DARTS_GROUP_PARAMS) {
   constexpr int esz = (EPI == EPI_F32 || EPI == EPI_ADD_F32) ? 4 : 2;
-  constexpr int BM = 256, BN = 256;
-  const int total = g.n_mtiles[0] * nt, chunk = (total + 7) >> 3;
+  const int total = n_mtiles[0] * nt, chunk = (total + 7) >> 3;
   const int hi = min(total, ((int)(blockIdx.x & 7) + 1) * chunk);
   int it = (int)(blockIdx.x & 7) * chunk + (int)(blockIdx.x >> 3);
   auto next = [&](AltItem& t) {
     if (it >= hi) return false;
-    const int mt = g.mtiles[it / nt], ni = it % nt;
+    const int mt = mtiles[it / nt], ni = it % nt;
     it += (int)(gridDim.x >> 3);
     const int e = mt >> 16, m0 = (mt & 0xffff) * BM;
-    const int64_t row = (int64_t)g.off[e] + m0;
-    t.a = (const bf16_t*)A + (g.arow ? 0 : row * K2);
+    const int64_t row = (int64_t)g_off[e] + m0;
+    t.a = (const bf16_t*)A + (arow ? 0 : row * lda2);
     t.w = (const bf16_t*)W + ((int64_t)e * N + ni * BN) * K2;
     t.c = (char*)C + (row * ldc + (EPI == EPI_SWIGLU ? ni * BN / 2 : ni * BN)) * esz;
-    t.rows = g.cnt[e] - m0;
-    t.arow = g.arow ? g.arow + row : nullptr;
+    t.rows = g_cnt[e] - m0;
+    t.arow = arow ? arow + row : nullptr;
     t.a_scale = a_scale + row;
     t.w_scale = w_scale + (int64_t)e * N + ni * BN;
     t.cols = N - ni * BN;
     return true;
   };
-  alt_gemm_items<I8Op, BM, BN, 2, 4, EPI, false, false>(K2, K2, ldc, K2 / 64, next);
+  alt_gemm_items<I8Op, BM, BN, 2, 4, EPI, false, false, WAUX, TAIL>(lda2, K2, ldc, (K2 + 127) / 128 * 2, next, K2);
 }
 
-// Row tile of a projection of `pairs` routed rows.  256 (alternating groups) from 97
-// rows per expert on, where K is whole pairs of K tiles and offsets (of gathered
-// rows: from the first one) fit 32 bits, else 128; below, 64.
-static int grouped_i8_rows(int64_t pairs, int E, int N, int K, int64_t gathered_bytes) {
-  if (pairs <= (int64_t)96 * E) return 64;
-  const bool fits = K % 256 == 0 && gathered_bytes < ((int64_t)1 << 32) &&
-                    (int64_t)256 * std::max<int64_t>(K, 2 * (int64_t)N) < ((int64_t)1 << 31);
-  return fits ? 256 : 128;
+// Row tile of the projections of `pairs` routed rows, by the rows per expert; 128
+// channels and two blocks per CU, or 256 channels in batches that give those blocks
+// work enough.  Layers in tiles of 128 x 128, 128 x 256 and 256 x 256, us: 128
+// experts (2048, 768), 8 each: 61 rows 115 / 120 / 160, 400 rows 133 / 132 / 169,
+// 976 rows (61 per expert) 167 / 158 / 195, 2000 rows (125) 265 / 244 / 227; 60
+// experts (1456, 720), 4 each: 61 rows 65 / 79 / 90, 976 rows (65) 92 / 101 / 107,
+// 2000 rows (133) 142 / 145 / 127.  (In tiles of 64 x 64 through a ring of LDS
+// stages 147, 180, 238, 370; 70, 110, 160.  With the weights straight into
+// registers and tiles of 16 to 96 rows 131, 172, 227 for 61, 400 and 976 rows of the
+// first.)
+constexpr int kI8TileRowsMin = 128;
+static int grouped_i8_rows(int64_t pairs, int E) { return pairs < (int64_t)100 * E ? kI8TileRowsMin : 256; }
+static bool grouped_i8_wide(int64_t pairs, int E, int N) {
+  return pairs >= (int64_t)24 * E && std::min<int64_t>(pairs, E) * ((N + 255) / 256) >= 2 * kI8Cus;
 }
 
-template <int BM, int BN, int STAGES, int BPC, int EPI>
-static hipError_t grouped_i8_go(const I8Call& c, const I8Groups& g, hipStream_t st) {
-  constexpr int lds = STAGES * (BM + BN) * 64 * 2;
-  auto kern = gemm_i8_grouped_kernel<BM, BN, STAGES, EPI>;
+template <int BM, int BN, int BPC, int EPI, int WAUX, bool TAIL>
+static hipError_t grouped_alt(const I8Call& c, const I8Groups& g, hipStream_t st) {
+  constexpr int lds = 2 * (BM + BN) * 64 * 2 + kAltScaleBytes;
+  auto kern = gemm_i8_alt_grouped_kernel<BM, BN, BPC, EPI, WAUX, TAIL>;
   static std::atomic<uint64_t> done{0};
   hipError_t e = allow_lds((const void*)kern, lds, done);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3(kI8Cus * BPC), dim3(256), lds, st, c.a, c.a_scale, c.w, c.w_scale, c.c, c.ldc, c.N, c.K / 2,
-                     (c.N + BN - 1) / BN, g);
+  hipLaunchKernelGGL(kern, dim3(kI8Cus * BPC), dim3(512), lds, st, c.a, c.a_scale, c.w, c.w_scale, c.c, c.ldc, c.N, c.K / 2,
+                     c.lda / 2, (c.N + BN - 1) / BN, DARTS_GROUP_ARGS(g));
   return hipGetLastError();
 }
+template <int BM, int BN, int BPC, int EPI, int WAUX>
+static hipError_t grouped_tail(const I8Call& c, const I8Groups& g, hipStream_t st) {
+  return c.K % 256 ? grouped_alt<BM, BN, BPC, EPI, WAUX, true>(c, g, st)
+                   : grouped_alt<BM, BN, BPC, EPI, WAUX, false>(c, g, st);
+}
+// c.M: the routed rows.
 template <int EPI>
-static hipError_t grouped_i8(int rows, const I8Call& c, const I8Groups& g, hipStream_t st) {
-  if (rows == 64) return grouped_i8_go<64, EPI == EPI_SWIGLU ? 64 : 128, EPI == EPI_SWIGLU ? 4 : 3, 2, EPI>(c, g, st);
-  if (rows == 128) return grouped_i8_go<128, 128, 2, 2, EPI>(c, g, st);
-  constexpr int lds = 2 * 512 * 64 * 2 + kAltScaleBytes;
-  auto kern = gemm_i8_alt_grouped_kernel<EPI>;
-  static std::atomic<uint64_t> done{0};
-  hipError_t e = allow_lds((const void*)kern, lds, done);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3(kI8Cus), dim3(512), lds, st, c.a, c.a_scale, c.w, c.w_scale, c.c, c.ldc, c.N, c.K / 2,
-                     (c.N + 255) / 256, g);
-  return hipGetLastError();
+static hipError_t grouped_i8(int rows, int E, const I8Call& c, const I8Groups& g, hipStream_t st) {
+  if (rows == 256) return grouped_tail<256, 256, 1, EPI, 0>(c, g, st);
+  return grouped_i8_wide(c.M, E, c.N) ? grouped_tail<128, 256, 1, EPI, kNtLoad>(c, g, st)
+                                      : grouped_tail<128, 128, 2, EPI, kNtLoad>(c, g, st);
 }
 
 // ------------------------------------------------------------ routed experts
@@ -646,6 +683,160 @@ __global__ void __launch_bounds__(256) combine_i8_kernel(const bf16_t* __restric
   }
 }
 
+// A few rows: nearly every (row, slot) pair has an expert of its own, so weights
+// are streamed per pair, without lists, in two launches that make the codes they
+// need themselves.  Lane (r, q) of a strip's load holds 16 codes of weight row r,
+// and every row of the matrix instruction's other operand is the pair's own.
+// Loads return in the order of their issue: the activations' come first, the
+// weights' are in flight while the codes are made.
+constexpr int kFewU = 4;                       // loads of 64 codes in one step
+struct FewStrip {
+  const int8_t* w;
+  int K;
+  i32x4_t b[2][kFewU], acc;
+  __device__ __forceinline__ void load(int k, int p) {
+    const int fq = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int u = 0; u < kFewU; ++u)
+      b[p][u] = __builtin_nontemporal_load((const i32x4_t*)(w + min(k + 64 * u + 16 * fq, K - 16)));
+  }
+  __device__ __forceinline__ void mma(const int8_t* q, int k, int ke, int p) {
+    const int fq = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int u = 0; u < kFewU; ++u)
+      if (k + 64 * u < ke) acc = I8Op::mma(*(const i32x4_t*)(q + k + 64 * u + 16 * fq), b[p][u], acc);
+  }
+  // the first loads of codes [kb, ke) (kb a multiple of 64), then their products
+  __device__ __forceinline__ void begin(const int8_t* w_, int K_, int kb) {
+    w = w_;
+    K = K_;
+    acc = (i32x4_t){0, 0, 0, 0};
+    __builtin_amdgcn_sched_barrier(0);
+    load(kb, 0);
+    load(kb + 64 * kFewU, 1);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __device__ __forceinline__ int sum(const int8_t* q, int kb, int ke) {
+    for (int k = kb; k < ke; k += 2 * 64 * kFewU) {
+      mma(q, k, ke, 0);
+      if (k + 2 * 64 * kFewU < ke) load(k + 2 * 64 * kFewU, 0);
+      mma(q, k + 64 * kFewU, ke, 1);
+      if (k + 3 * 64 * kFewU < ke) load(k + 3 * 64 * kFewU, 1);
+    }
+    return acc[0];
+  }
+};
+// A row of n <= 8 * T * N bf16 elements in the registers of T threads: its largest
+// magnitude (of a wavefront's part), and its codes into LDS, with zeros up to a
+// multiple of 64.
+template <int T, int N>
+struct FewRow {
+  X8<true> v[N];
+  __device__ __forceinline__ void load(const bf16_t* x, int n, int t) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i].v = (u32x4_t){0u, 0u, 0u, 0u};
+      if ((t + T * i) * 8 < n) v[i].load(x, (t + T * i) * 8);
+    }
+  }
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(v[i].at(e)) & 0x7fffffffu);
+    return wave_max_u32(m);
+  }
+  __device__ __forceinline__ void codes(float up, int n, int t, int8_t* q) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (t + T * i) * 8;
+      if (c >= (n + 63) / 64 * 64) continue;
+      uint32_t w[2] = {0u, 0u};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e >> 2] |= ((uint32_t)code_of(v[i].at(e), up) & 0xffu) << (8 * (e & 3));
+      *(uint2*)(q + c) = make_uint2(w[0], w[1]);
+    }
+  }
+};
+constexpr int kFewMaxD = 8192, kFewMaxFe = 2048;
+
+// h of one pair and 16 features: gate and up strips, four wavefronts each with a
+// quarter of K.
+__global__ void __launch_bounds__(512) few_gate_up_kernel(FfnI8Args a, bf16_t* __restrict__ h) {
+  extern __shared__ __attribute__((aligned(16))) int8_t q[];
+  __shared__ uint32_t tops[8];
+  __shared__ int32_t sums[8][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 15;
+  const int groups = a.Fe / 16, pair = blockIdx.x / groups, g = blockIdx.x % groups;
+  const int id = a.ids[pair];
+  FewRow<512, kFewMaxD / 4096> x;
+  x.load((const bf16_t*)a.x + (int64_t)(pair / a.k) * a.d, a.d, tid);
+  if (id < 0 || id >= a.E) return;
+  const int64_t row0 = (int64_t)id * 2 * a.Fe + g * 32;
+  const int kw = (a.d + 255) / 256 * 64, kb = min((wave & 3) * kw, a.d), ke = min(a.d, kb + kw);
+  FewStrip s;
+  s.begin(a.w_gu + (row0 + (wave >> 2) * 16 + fr) * a.d, a.d, kb);
+  const float s_gu = a.s_gu[row0 + (lane & 31)];
+  const uint32_t t = x.top();
+  if (lane == 0) tops[wave] = t;
+  __syncthreads();
+  uint32_t top = tops[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) top = max(top, tops[i]);
+  float up, scale;
+  row_scale(top, up, scale);
+  x.codes(up, a.d, tid, q);
+  __syncthreads();
+  const int sum = s.sum(q, kb, ke);
+  if (lane < 16) sums[wave][lane] = sum;
+  __syncthreads();
+  if (tid < 32) {
+    const int c = tid & 15, w = tid >> 4 << 2;
+    const float v = (float)(sums[w][c] + sums[w + 1][c] + sums[w + 2][c] + sums[w + 3][c]) * scale * s_gu;
+    const float u = __shfl_xor(v, 16, 64);
+    if (tid < 16) h[(int64_t)pair * a.Fe + g * 16 + tid] = f32_to_bf16(silu_f(v) * u);
+  }
+}
+
+// out of one row and 16 columns: wavefront w does the row's slots w, w + 8, ...
+template <int EPI>
+__global__ void __launch_bounds__(512) few_down_kernel(FfnI8Args a, const bf16_t* __restrict__ h) {
+  extern __shared__ __attribute__((aligned(16))) int8_t q[];
+  __shared__ float y[64][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 15;
+  const int strips = a.d / 16, r = blockIdx.x / strips, c0 = blockIdx.x % strips * 16;
+  int8_t* mine = q + wave * ((a.Fe + 63) / 64 * 64);
+  for (int j = wave; j < a.k; j += 8) {
+    const int id = a.ids[r * a.k + j];
+    float v = 0.f;
+    if (id >= 0 && id < a.E) {
+      FewRow<64, kFewMaxFe / 512> hr;
+      hr.load(h + ((int64_t)r * a.k + j) * a.Fe, a.Fe, lane);
+      const int64_t col = (int64_t)id * a.d + c0 + fr;
+      FewStrip s;
+      s.begin(a.w_down + col * a.Fe, a.Fe, 0);
+      const float s_down = a.s_down[col];
+      float up, scale;
+      row_scale(hr.top(), up, scale);
+      hr.codes(up, a.Fe, lane, mine);
+      __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): only this wavefront reads them
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      v = bf16_to_f32(f32_to_bf16((float)s.sum(mine, 0, a.Fe) * scale * s_down));
+    }
+    if (lane < 16) y[j][lane] = v;
+  }
+  __syncthreads();
+  if (tid < 16) {
+    float s = 0.f;
+    for (int j = 0; j < a.k; ++j) s = fmaf(a.weights[r * a.k + j], y[j][tid], s);
+    epi_store<EPI>(a.out, a.d, INT32_MAX, r, c0 + tid, s);
+  }
+}
+
+// Codes' rows in the workspace: whole pairs of K tiles.
+static int64_t padded(int64_t k) { return (k + 255) / 256 * 256; }
 // Workspace of the expert layer, in this order, each part 256-byte aligned.
 struct FfnWork {
   int8_t *q, *hq;
@@ -662,20 +853,20 @@ static size_t ffn_layout(int64_t rows, int d, int E, int k, int Fe, char* base, 
   };
   const size_t pairs = (size_t)rows * k;
   FfnWork t;
-  t.q = (int8_t*)part((size_t)rows * d);
+  t.q = (int8_t*)part((size_t)rows * padded(d));
   t.q_scale = (float*)part((size_t)rows * 4);
   t.pos_scale = (float*)part(pairs * 4);
   t.counts = (int32_t*)part((size_t)E * 4);
   t.offsets = (int32_t*)part((size_t)E * 4);
-  t.mtiles = (int32_t*)part((pairs / kGroupedTileRowsMin + E) * 4);
+  t.mtiles = (int32_t*)part((pairs / kI8TileRowsMin + E) * 4);
   t.n_mtiles = (int32_t*)part(4);
-  t.mtiles_dn = (int32_t*)part((pairs / kGroupedTileRowsMin + E) * 4);
+  t.mtiles_dn = (int32_t*)part((pairs / kI8TileRowsMin + E) * 4);
   t.n_mtiles_dn = (int32_t*)part(4);
   t.blk = (int32_t*)part((size_t)kMoeBlocks * E * 4);
   t.pos_of = (int32_t*)part(pairs * 4);
   t.row_of = (int32_t*)part(pairs * 4);
   t.h = (bf16_t*)part(pairs * Fe * 2);
-  t.hq = (int8_t*)part(pairs * Fe);
+  t.hq = (int8_t*)part(pairs * padded(Fe));
   t.h_scale = (float*)part(pairs * 4);
   t.y = (bf16_t*)part(pairs * d * 2);
   if (f) *f = t;
@@ -685,28 +876,46 @@ size_t moe_ffn_i8_workspace_bytes(int64_t rows, int d, int E, int k, int Fe) {
   return ffn_layout(rows, d, E, k, Fe, nullptr, nullptr);
 }
 
+// Whether weights are streamed per pair: while pairs share few experts, or read so
+// little that launches are the cost.  Two launches against lists, us: 128 experts
+// (2048, 768), 8 each: 1 row 15.6 / 30, 4 rows 33 / 46, 8 rows 60 / 64; 64 experts
+// (1024, 1408), 6 each: 4 rows 34 / 40, 6 rows 51 / 47; 16 experts (1024, 512), 4
+// each: 1 row 11 / 24, 8 rows 18 / 26, 12 rows 26 / 26.
+static bool few_rows(const FfnI8Args& a) {
+  const int64_t pairs = (int64_t)a.n_rows * a.k;
+  return (2 * pairs <= a.E || 3 * pairs * a.d * a.Fe <= 60000000) && a.d <= kFewMaxD && a.Fe <= kFewMaxFe;
+}
+
 hipError_t launch_moe_ffn_i8(const FfnI8Args& a, hipStream_t st) {
   if (a.n_rows <= 0) return hipSuccess;
   FfnWork f;
   if (ffn_layout(a.n_rows, a.d, a.E, a.k, a.Fe, (char*)a.ws, &f) > a.ws_bytes) return hipErrorInvalidValue;
-  hipError_t e = launch_quantize_rows(a.x, a.n_rows, a.d, a.d, true, f.q, f.q_scale, st);
-  if (e != hipSuccess) return e;
   const int n_pairs = a.n_rows * a.k;
+  if (few_rows(a)) {
+    hipLaunchKernelGGL(few_gate_up_kernel, dim3(n_pairs * (a.Fe / 16)), dim3(512), (a.d + 63) / 64 * 64, st, a, f.h);
+    const dim3 grid(a.n_rows * (a.d / 16));
+    const int lds = 8 * ((a.Fe + 63) / 64 * 64);
+    if (a.epi == EPI_ADD_F32) hipLaunchKernelGGL(few_down_kernel<EPI_ADD_F32>, grid, dim3(512), lds, st, a, f.h);
+    else hipLaunchKernelGGL(few_down_kernel<EPI_BF16>, grid, dim3(512), lds, st, a, f.h);
+    return hipGetLastError();
+  }
+  hipError_t e = launch_quantize_rows(a.x, a.n_rows, a.d, a.d, true, f.q, padded(a.d), f.q_scale, st);
+  if (e != hipSuccess) return e;
   MoeListArgs l{};
   l.topk_id = a.ids; l.n_pairs = n_pairs; l.E = a.E; l.k = a.k;
   l.counts = f.counts; l.offsets = f.offsets;
   l.mtiles = f.mtiles; l.n_mtiles = f.n_mtiles; l.mtiles_dn = f.mtiles_dn; l.n_mtiles_dn = f.n_mtiles_dn;
-  l.tile_rows = grouped_i8_rows(n_pairs, a.E, 2 * a.Fe, a.d, (int64_t)a.n_rows * a.d);
-  l.tile_rows_dn = grouped_i8_rows(n_pairs, a.E, a.d, a.Fe, 0);
+  const int tile = grouped_i8_rows(n_pairs, a.E);
+  l.tile_rows = l.tile_rows_dn = tile;
   l.blk = f.blk; l.pos_of = f.pos_of; l.row_of = f.row_of;
   l.row_scale = f.q_scale; l.pos_scale = f.pos_scale;
   if ((e = launch_moe_lists(l, st)) != hipSuccess) return e;
-  const I8Call gu{f.q, f.pos_scale, a.w_gu, a.s_gu, f.h, 0, 2 * a.Fe, a.d, a.Fe, nullptr};
-  if ((e = grouped_i8<EPI_SWIGLU>(l.tile_rows, gu, {f.offsets, f.counts, f.mtiles, f.n_mtiles, f.row_of}, st)) != hipSuccess)
+  const I8Call gu{f.q, f.pos_scale, a.w_gu, a.s_gu, f.h, n_pairs, 2 * a.Fe, a.d, (int)padded(a.d), a.Fe, nullptr};
+  if ((e = grouped_i8<EPI_SWIGLU>(tile, a.E, gu, {f.offsets, f.counts, f.mtiles, f.n_mtiles, f.row_of}, st)) != hipSuccess)
     return e;
-  if ((e = launch_quantize_rows(f.h, n_pairs, a.Fe, a.Fe, true, f.hq, f.h_scale, st)) != hipSuccess) return e;
-  const I8Call dn{f.hq, f.h_scale, a.w_down, a.s_down, f.y, 0, a.d, a.Fe, a.d, nullptr};
-  if ((e = grouped_i8<EPI_BF16>(l.tile_rows_dn, dn, {f.offsets, f.counts, f.mtiles_dn, f.n_mtiles_dn, nullptr}, st)) != hipSuccess)
+  if ((e = launch_quantize_rows(f.h, n_pairs, a.Fe, a.Fe, true, f.hq, padded(a.Fe), f.h_scale, st)) != hipSuccess) return e;
+  const I8Call dn{f.hq, f.h_scale, a.w_down, a.s_down, f.y, n_pairs, a.d, a.Fe, (int)padded(a.Fe), a.d, nullptr};
+  if ((e = grouped_i8<EPI_BF16>(tile, a.E, dn, {f.offsets, f.counts, f.mtiles_dn, f.n_mtiles_dn, nullptr}, st)) != hipSuccess)
     return e;
   if (a.epi == EPI_ADD_F32)
     hipLaunchKernelGGL(combine_i8_kernel<EPI_ADD_F32>, dim3(a.n_rows), dim3(256), 0, st, f.y, a.d, a.k, f.pos_of,

@@ -211,26 +211,51 @@ __device__ __forceinline__ void moe_place(const int32_t* __restrict__ topk_id, i
 }
 
 // Decode batches: everything in a single block, counts by an LDS histogram of
-// the n_pairs routed (row, slot) pairs.
+// the n_pairs routed (row, slot) pairs.  A thread keeps its pairs' experts and
+// their places among the expert's pairs (what the histogram's adds return) in
+// registers, so ids are read once and there is one round of atomics: 7808 pairs
+// 9 us, 18 us when they were read and counted again to be placed.
+constexpr int kMoeOneBlockPairs = 16384;
 __global__ void __launch_bounds__(1024) moe_offsets_kernel(const int32_t* __restrict__ topk_id, int n_pairs, int E,
                                                            int k, MoeLists lists, int32_t* __restrict__ pos_of,
                                                            int32_t* __restrict__ row_of,
                                                            const float* __restrict__ row_scale,
                                                            float* __restrict__ pos_scale) {
+  constexpr int N = kMoeOneBlockPairs / 1024;
   __shared__ int32_t hist[1024];
   __shared__ int32_t sh[32];
   const int tid = threadIdx.x;
+  int e[N], at[N];
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    e[u] = -1;
+    if (1024 * u < n_pairs && tid + 1024 * u < n_pairs) e[u] = topk_id[tid + 1024 * u];
+  }
   hist[tid] = 0;
   __syncthreads();
-  for (int i = tid; i < n_pairs; i += 1024) {
-    const int e = topk_id[i];
-    if (e >= 0 && e < E) atomicAdd(&hist[e], 1);
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    if (1024 * u >= n_pairs) break;
+    at[u] = -1;
+    if (e[u] >= 0 && e[u] < E) at[u] = atomicAdd(&hist[e[u]], 1);
   }
   __syncthreads();
   const int ex = moe_lists(lists, tid < E ? hist[tid] : 0, E, sh);
-  hist[tid] = tid < E ? ex : 0;          // the per-expert cursors
+  hist[tid] = tid < E ? ex : 0;          // the experts' first positions
   __syncthreads();
-  moe_place(topk_id, 0, n_pairs, E, k, hist, pos_of, row_of, row_scale, pos_scale);
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const int i = tid + 1024 * u;
+    if (1024 * u >= n_pairs) break;
+    if (i >= n_pairs) continue;
+    int p = -1;
+    if (at[u] >= 0) {
+      p = hist[e[u]] + at[u];
+      row_of[p] = i / k;
+      if (pos_scale) pos_scale[p] = row_scale[i / k];
+    }
+    pos_of[i] = p;
+  }
 }
 
 // Large batches (the prefill): the pairs go to kMoeBlocks blocks, which count
@@ -239,7 +264,6 @@ __global__ void __launch_bounds__(1024) moe_offsets_kernel(const int32_t* __rest
 // prefill of 32768 rows x 8: 21 us in all, 228 us in a single block, whose LDS
 // atomics are the bound; up to kMoeOneBlockPairs pairs the single block takes
 // about as long as the three launches.
-constexpr int kMoeOneBlockPairs = 16384;
 __device__ __forceinline__ int moe_block_begin(int b, int n_pairs) { return (int)((int64_t)n_pairs * b / kMoeBlocks); }
 __global__ void __launch_bounds__(1024) moe_count_kernel(const int32_t* __restrict__ topk_id, int n_pairs, int E,
                                                          int32_t* __restrict__ blk) {

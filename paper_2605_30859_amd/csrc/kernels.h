@@ -295,8 +295,9 @@ struct RouteArgs {
 hipError_t launch_route(const RouteArgs& a, hipStream_t st);
 
 // ---- 8-bit integers (k_i8.hip)
-hipError_t launch_quantize_rows(const void* x, int64_t rows, int cols, int64_t ldx, bool bf16, int8_t* q, float* scale,
-                                hipStream_t st);
+// codes ldq apart, zeros between them (ldq beyond cols: whole 16-byte pieces only)
+hipError_t launch_quantize_rows(const void* x, int64_t rows, int cols, int64_t ldx, bool bf16, int8_t* q, int64_t ldq,
+                                float* scale, hipStream_t st);
 size_t gemm_i8_workspace_bytes(int M, int N, int K);
 hipError_t launch_gemm_i8(const int8_t* a, const float* a_scale, const int8_t* w, const float* w_scale, void* c, int M,
                           int N, int K, int epi, void* ws, size_t ws_bytes, hipStream_t st);

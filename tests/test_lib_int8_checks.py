@@ -46,7 +46,7 @@ def test_product_refusals(lib):
     def call(M=4, n=64, K=64, epi=0, a=D, sa=D, w=D, sw=D, c=D):
         return lib.darts_gemm_i8(a, sa, w, sw, c, M, n, K, epi, N, 0, N)
     for kw in (dict(M=-1), dict(n=0), dict(n=40), dict(K=0), dict(K=72), dict(K=131072 + 16), dict(epi=4), dict(epi=-1),
-               dict(n=48, epi=3), dict(a=N), dict(sa=N), dict(w=N), dict(sw=N), dict(c=N), dict(a=ODD), dict(w=ODD)):
+               dict(n=48, epi=3), dict(M=1 << 30, n=1 << 16), dict(a=N), dict(sa=N), dict(w=N), dict(sw=N), dict(c=N), dict(a=ODD), dict(w=ODD)):
         assert call(**kw) == EINVAL, kw
     # a plan that needs a workspace, without one and with one too small
     for M, n, K in ((1, 4096, 12288), (45, 4096, 12288), (200, 2048, 4096), (16, 1024, 4096)):
