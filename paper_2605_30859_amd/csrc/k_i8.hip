@@ -179,12 +179,14 @@ hipError_t launch_quantize_rows(const void* x, int64_t rows, int cols, int64_t l
 // Up to 16 * MT rows.  WK wavefronts share a strip of 16 channels, each a range of
 // kw codes of K (a multiple of 64), and a block has 8 / WK strips.  Lane (r, q)
 // loads 16 codes of row r; the loads of U steps of 64 are issued before the
-// products of the U steps before.
+// products of the U steps before.  (One row, 6144 x 4096 from memory: 7.7 us with U
+// 2, 7.9 with 4, 7.6 with 8, 24576 x 4096 19.9, 22.7, 20.9; non-temporal loads 8.6
+// and 25 us with U 4, and 20-40% behind where a cache holds the weights.)
 template <int MT, int WK, int EPI>
 __global__ void __launch_bounds__(512) gemm_i8_skinny_kernel(const int8_t* __restrict__ A, const float* __restrict__ a_scale,
                                                              const int8_t* __restrict__ W, const float* __restrict__ w_scale,
                                                              void* __restrict__ C, int ldc, int M, int N, int K, int kw) {
-  constexpr int U = 4, NS = 8 / WK;
+  constexpr int U = 2, NS = 8 / WK;
   static_assert(EPI != EPI_SWIGLU || NS % 2 == 0, "gate and up strips in one block");
   __shared__ i32x4_t red[8][MT][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, fq = lane >> 4;
@@ -202,7 +204,7 @@ __global__ void __launch_bounds__(512) gemm_i8_skinny_kernel(const int8_t* __res
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int at = min(k + 64 * u + 16 * fq, ke - 16);
-      b[p][u] = __builtin_nontemporal_load((const i32x4_t*)(wp + at));
+      b[p][u] = *(const i32x4_t*)(wp + at);
 #pragma unroll
       for (int i = 0; i < MT; ++i) a[p][u][i] = *(const i32x4_t*)(ap[i] + at);
     }
@@ -384,14 +386,15 @@ static double i8_estimate(const I8Plan& p, int M, int N, int K) {
 }
 
 // Skinny: a few rows; up to 16 of them while the weights are small (16 rows: 4096 x
-// 4096 8.0 us against 9.1 in tiles, 6144 x 4096 12.1 against 10.9), up to 32 while
-// K is short, too (32 rows: 8192 x 1024 6.0 against 6.6, 2048 x 4096 9.2 against
-// 8.7).  Eight wavefronts per strip, or four of twice the range where the strips
-// alone give enough of them (one row: 6144 x 4096 8.5 us with four, 9.4 with
-// eight; 2048 x 4096 7.8 and 5.3; 12288 x 8192 25 and 20.7).
+// 4096 6.9 us against 9.1 in tiles, 6144 x 4096 10.5 against 10.9, 4096 x 12288 15.6
+// against 15.1, 24576 x 4096 30 against 23), up to 32 while K is short, too (32 rows:
+// 8192 x 1024 6.0 against 6.6, 2048 x 4096 9.2 against 8.7).  Eight wavefronts per
+// strip, or four of twice the range where the strips alone give enough of them (one
+// row: 6144 x 4096 7.7 us with four, 8.2 with eight; 2048 x 4096 6.9 and 5.1; 12288 x
+// 8192 23 and 20).
 static bool skinny_i8_plan(I8Plan& p, int M, int N, int K) {
   const int64_t w = (int64_t)N * K;
-  if (M > 4 && !(M <= 16 && w <= 20000000) && !(M <= 32 && w <= 8400000 && K <= 2048)) return false;
+  if (M > 4 && !(M <= 16 && w <= 26000000) && !(M <= 32 && w <= 8400000 && K <= 2048)) return false;
   return set_i8_plan(p, -1, N >= 16 * 384 && K <= 4096 ? 4 : 8, M, N, K);
 }
 
@@ -643,7 +646,8 @@ static hipError_t grouped_i8(int rows, int E, const I8Call& c, const I8Groups& g
 
 // ------------------------------------------------------------ routed experts
 // out[r] = sum_j w[r][j] * y[pos(r, j)] in slot order, fp32 sums, 8 columns per
-// thread.  A place without an expert adds w * 0: nothing, or NaN for the weight
+// thread; y is read once, non-temporal (a layer of 8000 rows 482 us, 590 with plain
+// loads; 32768 rows 1657 and 1785).  A place without an expert adds w * 0: nothing, or NaN for the weight
 // NaN of a row that the router could not read.
 template <int EPI>
 __global__ void __launch_bounds__(256) combine_i8_kernel(const bf16_t* __restrict__ y, int d, int k,
@@ -663,7 +667,7 @@ __global__ void __launch_bounds__(256) combine_i8_kernel(const bf16_t* __restric
         if (j0 + j < k) {
           const int p = pos_of[r * k + j0 + j];
           wj[j] = weights[r * k + j0 + j];
-          if (p >= 0) v[j].load(y, (int64_t)p * d + c);
+          if (p >= 0) v[j].v = __builtin_nontemporal_load((const u32x4_t*)(y + (int64_t)p * d + c));
         }
       }
 #pragma unroll
@@ -689,7 +693,7 @@ __global__ void __launch_bounds__(256) combine_i8_kernel(const bf16_t* __restric
 // and every row of the matrix instruction's other operand is the pair's own.
 // Loads return in the order of their issue: the activations' come first, the
 // weights' are in flight while the codes are made.
-constexpr int kFewU = 4;                       // loads of 64 codes in one step
+constexpr int kFewU = 2;                       // loads of 64 codes in one step (one row of 128 experts: 13.0 us, with 4 13.4, with 8 17.0)
 struct FewStrip {
   const int8_t* w;
   int K;
@@ -698,7 +702,7 @@ struct FewStrip {
     const int fq = (threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int u = 0; u < kFewU; ++u)
-      b[p][u] = __builtin_nontemporal_load((const i32x4_t*)(w + min(k + 64 * u + 16 * fq, K - 16)));
+      b[p][u] = *(const i32x4_t*)(w + min(k + 64 * u + 16 * fq, K - 16));
   }
   __device__ __forceinline__ void mma(const int8_t* q, int k, int ke, int p) {
     const int fq = (threadIdx.x & 63) >> 4;
@@ -878,12 +882,13 @@ size_t moe_ffn_i8_workspace_bytes(int64_t rows, int d, int E, int k, int Fe) {
 
 // Whether weights are streamed per pair: while pairs share few experts, or read so
 // little that launches are the cost.  Two launches against lists, us: 128 experts
-// (2048, 768), 8 each: 1 row 15.6 / 30, 4 rows 33 / 46, 8 rows 60 / 64; 64 experts
-// (1024, 1408), 6 each: 4 rows 34 / 40, 6 rows 51 / 47; 16 experts (1024, 512), 4
-// each: 1 row 11 / 24, 8 rows 18 / 26, 12 rows 26 / 26.
+// (2048, 768), 8 each: 1 row 13 / 32, 4 rows 30 / 46, 10 rows 64 / 68; 64 experts
+// (1024, 1408), 6 each: 4 rows 24 / 39, 7 rows 35 / 49; 60 experts (1456, 720), 4
+// each: 10 rows 30 / 48; 16 experts (1024, 512), 4 each: 1 row 8 / 25, 15 rows 18 / 27.
 static bool few_rows(const FfnI8Args& a) {
   const int64_t pairs = (int64_t)a.n_rows * a.k;
-  return (2 * pairs <= a.E || 3 * pairs * a.d * a.Fe <= 60000000) && a.d <= kFewMaxD && a.Fe <= kFewMaxFe;
+  return (3 * pairs <= 2 * a.E || (pairs <= 72 && 3 * pairs * a.d * a.Fe <= 250000000)) && a.d <= kFewMaxD &&
+         a.Fe <= kFewMaxFe;
 }
 
 hipError_t launch_moe_ffn_i8(const FfnI8Args& a, hipStream_t st) {

@@ -164,11 +164,12 @@ struct MoeLists {
   int tile_rows, tile_rows2;
 };
 // The lists from thread e's count v of expert e (0 for e >= E), by one block of
-// 1024 threads; returns the expert's offset.
-__device__ __forceinline__ int moe_lists(const MoeLists& l, int v, int E, int32_t* sh) {
+// 1024 threads; returns the expert's offset.  write: the same in the whole block.
+__device__ __forceinline__ int moe_lists(const MoeLists& l, int v, int E, int32_t* sh, bool write = true) {
   const int tid = threadIdx.x;
   int total;
   const int ex = block_excl_scan1024(v, sh, &total);
+  if (!write) return ex;
   const int nt = (v + l.tile_rows - 1) / l.tile_rows;
   int ntiles;
   const int tex = block_excl_scan1024(nt, sh, &ntiles);
@@ -210,11 +211,14 @@ __device__ __forceinline__ void moe_place(const int32_t* __restrict__ topk_id, i
   }
 }
 
-// Decode batches: everything in a single block, counts by an LDS histogram of
-// the n_pairs routed (row, slot) pairs.  A thread keeps its pairs' experts and
-// their places among the expert's pairs (what the histogram's adds return) in
-// registers, so ids are read once and there is one round of atomics: 7808 pairs
-// 9 us, 18 us when they were read and counted again to be placed.
+// Decode batches: one launch, counts by an LDS histogram of the n_pairs routed
+// (row, slot) pairs.  A thread keeps its pairs' experts and their places among the
+// expert's pairs (what the histogram's adds return) in registers.  Every block
+// counts all pairs, the first writes the lists, and each places the pairs of its
+// own share of the experts: the stores to 64 different lines per instruction are
+// what placing costs (7808 pairs 18 us in one block that counted twice, 15 in one
+// that counted once).
+constexpr int kMoePlaceBlocks = 16, kMoePlaceAlone = 512;   // blocks, from so many pairs on
 constexpr int kMoeOneBlockPairs = 16384;
 __global__ void __launch_bounds__(1024) moe_offsets_kernel(const int32_t* __restrict__ topk_id, int n_pairs, int E,
                                                            int k, MoeLists lists, int32_t* __restrict__ pos_of,
@@ -240,21 +244,23 @@ __global__ void __launch_bounds__(1024) moe_offsets_kernel(const int32_t* __rest
     if (e[u] >= 0 && e[u] < E) at[u] = atomicAdd(&hist[e[u]], 1);
   }
   __syncthreads();
-  const int ex = moe_lists(lists, tid < E ? hist[tid] : 0, E, sh);
+  const int ex = moe_lists(lists, tid < E ? hist[tid] : 0, E, sh, blockIdx.x == 0);
   hist[tid] = tid < E ? ex : 0;          // the experts' first positions
   __syncthreads();
+  const int lo = (int)(blockIdx.x * E / gridDim.x), hi = (int)((blockIdx.x + 1) * E / gridDim.x);
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     const int i = tid + 1024 * u;
     if (1024 * u >= n_pairs) break;
     if (i >= n_pairs) continue;
-    int p = -1;
-    if (at[u] >= 0) {
-      p = hist[e[u]] + at[u];
+    if (at[u] < 0) {
+      if (blockIdx.x == 0) pos_of[i] = -1;
+    } else if (e[u] >= lo && e[u] < hi) {
+      const int p = hist[e[u]] + at[u];
       row_of[p] = i / k;
       if (pos_scale) pos_scale[p] = row_scale[i / k];
+      pos_of[i] = p;
     }
-    pos_of[i] = p;
   }
 }
 
@@ -402,7 +408,7 @@ hipError_t launch_moe_lists(const MoeListArgs& a, hipStream_t st) {
   const MoeLists lists{a.counts, a.offsets, a.mtiles, a.n_mtiles, a.mtiles_dn, a.n_mtiles_dn, a.touched_out,
                        a.tile_rows, a.tile_rows_dn};
   if (a.n_pairs <= kMoeOneBlockPairs) {
-    hipLaunchKernelGGL(moe_offsets_kernel, dim3(1), dim3(1024), 0, st, a.topk_id, a.n_pairs, a.E, a.k, lists, a.pos_of,
+    hipLaunchKernelGGL(moe_offsets_kernel, dim3(a.n_pairs < kMoePlaceAlone ? 1 : kMoePlaceBlocks), dim3(1024), 0, st, a.topk_id, a.n_pairs, a.E, a.k, lists, a.pos_of,
                        a.row_of, a.row_scale, a.pos_scale);
   } else {
     hipLaunchKernelGGL(moe_count_kernel, dim3(kMoeBlocks), dim3(1024), 0, st, a.topk_id, a.n_pairs, a.E, a.blk);
