@@ -321,6 +321,17 @@ __device__ __forceinline__ void dma_gemm_tile(const bf16_t* __restrict__ A, int 
   }
 }
 
+// 16 bytes to buffer r at voff + soff. A vector instruction that writes one of
+// the last three data registers right after such a store can still change what
+// is stored (seen here: accumulators, converted for the next store, in memory
+// in place of results). The compiler puts the two wait states between them only
+// where soff is a constant, so they stand here, and the data, an input of the
+// same statement, keeps its registers until then.
+__device__ __forceinline__ void store_b128(u32x4_t v, __amdgpu_buffer_rsrc_t r, int voff, int soff) {
+  __builtin_amdgcn_raw_buffer_store_b128(v, r, voff, soff, 0);
+  asm volatile("s_nop 1" ::"v"(v) : "memory");
+}
+
 // ------------------------------------------------------- alternating groups
 // BM x BN output tile for compute-bound launches: 8 wavefronts in two groups
 // of four (one wavefront of each group per SIMD) that alternate between
@@ -696,7 +707,7 @@ __device__ __forceinline__ void alt_gemm_items(int lda, int ldw, int ldc, int nk
             const int o = (m * ldc + ((kSwiglu ? wn : 2 * wn + g) * TN + j) * 16) * kEsz;
             if (!inside(g, j)) continue;
             if constexpr (kPair)
-              __builtin_amdgcn_raw_buffer_store_b128((u32x4_t){v[j].x, v[j].y, v[j + 1].x, v[j + 1].y}, cres, cvoff, o, 0);
+              store_b128((u32x4_t){v[j].x, v[j].y, v[j + 1].x, v[j + 1].y}, cres, cvoff, o);
             else
               __builtin_amdgcn_raw_buffer_store_b64((u32x2_t){v[j].x, v[j].y}, cres, cvoff, o, 0);
           }
@@ -719,8 +730,8 @@ __device__ __forceinline__ void alt_gemm_items(int lda, int ldw, int ldc, int nk
             if (!inside(g, j)) continue;
             f32x4_t v = value(h, g, i, j);
             if constexpr (!SPLIT && EPI == EPI_ADD_F32) v += r[g][j];
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), cres, cvoff,
-                                                   (m * ldc + ((kSwiglu ? wn : 2 * wn + g) * TN + j) * 16) * kEsz, 0);
+            store_b128(__builtin_bit_cast(u32x4_t, v), cres, cvoff,
+                       (m * ldc + ((kSwiglu ? wn : 2 * wn + g) * TN + j) * 16) * kEsz);
           }
       }
     };
