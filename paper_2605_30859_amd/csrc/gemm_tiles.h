@@ -25,7 +25,7 @@ struct Bf16Op {
   }
 };
 // Codes: sums in 32-bit integers, exact.  a_scale[m] belongs to row m of the
-// output (also where its A row is gathered), w_scale[n] to its column n.  N is any
+// output, w_scale[n] to its column n.  N is any
 // multiple of 16, K (in codes) of 16: the ring fills the last K tile with zeros
 // past klen units, and columns past N repeat W's last row and are not stored.
 struct I8Op {
@@ -390,8 +390,9 @@ struct AltItem {
   char* c;               // its first output element
   int rows;              // rows of the output from the tile's first one on (> 0)
   const int32_t* arow;   // NULL, or the A row of each of them
-  // codes: the scales of the tile's first row and first column of W, and W's rows
-  // from the tile's first one on (a multiple of 16, > 0)
+  // codes: the scales of A's rows (as arow counts them, else from the tile's first
+  // row) and of the tile's first column of W, and W's rows from the tile's first one
+  // on (a multiple of 16, > 0)
   const float *a_scale, *w_scale;
   int cols;
 };
@@ -448,7 +449,15 @@ __device__ __forceinline__ void alt_gemm_items(int lda, int ldw, int ldc, int nk
   constexpr bool kPair = kEsz == 2 && TN % 2 == 0;
   const int wlane = kPair ? 8 * (lrow >> 2) + (lrow & 3) : lrow;   // row in a strip of 16, but for a uniform part
   int woff = PW ? ((gchunk & 3) * 16 + wlane) * 16 + (gchunk >> 2) * 1024 : (wlane * ldw + gchunk * 8) * 2;
+  constexpr bool kScales = Op::kI8 && !SPLIT;
+  [[maybe_unused]] int srow = 0;                      // codes: the row whose scale this lane fetches
   auto row_ids = [&](const AltItem& t, int (&row)[2][LA]) {
+    if constexpr (kScales) {
+      int s = lane + 64 * (wave & 3);
+      asm volatile("" : "+v"(s));
+      s = min(s, t.rows - 1);
+      srow = t.arow && first ? t.arow[s] : s;
+    }
     int row0 = lrow;
     asm volatile("" : "+v"(row0));                    // recomputed here, not kept over the K loop
 #pragma unroll
@@ -599,7 +608,6 @@ __device__ __forceinline__ void alt_gemm_items(int lda, int ldw, int ldc, int nk
   // Codes: an item's scales (of its 256 rows, then of its channels) go to LDS
   // with its first loads, into one of two places by turns, since that is before
   // the results of the item before are scaled.
-  constexpr bool kScales = Op::kI8 && !SPLIT;
   [[maybe_unused]] float* scales = (float*)(smem + 4 * (HA + HB));
   [[maybe_unused]] int turn = 0;
   // the first loads of cur, whose rows are in arow
@@ -609,7 +617,7 @@ __device__ __forceinline__ void alt_gemm_items(int lda, int ldw, int ldc, int nk
     if constexpr (kScales) {
       int t = lane + 64 * (wave & 3);
       asm volatile("" : "+v"(t));                     // recomputed here, not kept over the K loop
-      const float* src = first ? cur.a_scale + min(t, cur.rows - 1) : cur.w_scale + min(t, min(cur.cols, BN) - 1);
+      const float* src = first ? cur.a_scale + srow : cur.w_scale + min(t, min(cur.cols, BN) - 1);
       __builtin_amdgcn_global_load_lds((const void*)src, (lds_void_t*)(scales + turn * 512 + wave * 64), 4, 0, 0);
     }
 #pragma unroll

@@ -14,6 +14,7 @@
 #include "common.h"
 #include "gemm_tiles.h"
 #include "kernels.h"
+#include "moe_lists.h"
 
 namespace darts {
 
@@ -70,14 +71,9 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 // rows of up to 64 * WPR * 32 elements are read once.
 constexpr int kQuantKeep = 4;
 template <bool BF16, bool VEC, int WPR>
-__global__ void __launch_bounds__(256) quantize_rows_kernel(const void* __restrict__ x, int64_t rows, int cols, int64_t ldx,
-                                                            int8_t* __restrict__ q, int64_t ldq,
-                                                            float* __restrict__ scale) {
-  __shared__ uint32_t red[4];
-  constexpr int T = 64 * WPR;                          // threads of a row
-  const int64_t r = (int64_t)blockIdx.x * (4 / WPR) + threadIdx.x / T;
-  const int t = threadIdx.x % T;
-  if (WPR == 1 && r >= rows) return;
+__device__ __forceinline__ void quantize_row(const void* __restrict__ x, int64_t r, int t, uint32_t* red, int cols, int64_t ldx,
+                                             int8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale) {
+  constexpr int T = 64 * WPR;                          // threads of the row
   X8<BF16> keep[kQuantKeep];
   uint32_t top = 0;
   const int n8 = cols / 8;
@@ -100,7 +96,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const void* __restri
     for (int c = t; c < cols; c += T) top = max(top, __float_as_uint(load_x<BF16>(x, r * ldx + c)) & 0x7fffffffu);
   }
   top = wave_max_u32(top);
-  if constexpr (WPR == 4) {
+  if constexpr (WPR == 4) {                            // in a block, every row at once
     if ((t & 63) == 0) red[t >> 6] = top;
     __syncthreads();
     top = max(max(red[0], red[1]), max(red[2], red[3]));
@@ -131,6 +127,16 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const void* __restri
   } else {
     for (int c = t; c < cols; c += T) q[r * ldq + c] = (int8_t)code_of(load_x<BF16>(x, r * ldx + c), up);
   }
+}
+
+template <bool BF16, bool VEC, int WPR>
+__global__ void __launch_bounds__(256) quantize_rows_kernel(const void* __restrict__ x, int64_t rows, int cols, int64_t ldx,
+                                                            int8_t* __restrict__ q, int64_t ldq,
+                                                            float* __restrict__ scale) {
+  __shared__ uint32_t red[4];
+  const int64_t r = (int64_t)blockIdx.x * (4 / WPR) + threadIdx.x / (64 * WPR);
+  if (r >= rows) return;                               // the whole wavefront; with WPR 4 no block has any
+  quantize_row<BF16, VEC, WPR>(x, r, threadIdx.x % (64 * WPR), red, cols, ldx, q, ldq, scale);
 }
 
 template <bool BF16, bool VEC>
@@ -560,8 +566,8 @@ hipError_t launch_gemm_i8(const int8_t* a, const float* a_scale, const int8_t* w
 }
 
 // ------------------------------------------------------------------- grouped
-// Expert e owns rows [off[e], off[e] + cnt[e]) of C and of a_scale, and of A or of
-// the row list into A; mtiles lists the non-empty row tiles (e << 16 | tile).
+// Expert e owns rows [off[e], off[e] + cnt[e]) of C, and of A and a_scale or of the
+// row list into them; mtiles lists the non-empty row tiles (e << 16 | tile).
 // Persistent blocks take items (row tile, column tile), column tile fastest; each
 // XCD takes a contiguous eighth of them, so the column tiles of an expert's row
 // tile find its rows in that XCD's L2.
@@ -596,7 +602,7 @@ __global__ void __launch_bounds__(512, 2 * BPC)
     t.c = (char*)C + (row * ldc + (EPI == EPI_SWIGLU ? ni * BN / 2 : ni * BN)) * esz;
     t.rows = g_cnt[e] - m0;
     t.arow = arow ? arow + row : nullptr;
-    t.a_scale = a_scale + row;
+    t.a_scale = arow ? a_scale : a_scale + row;
     t.w_scale = w_scale + (int64_t)e * N + ni * BN;
     t.cols = N - ni * BN;
     return true;
@@ -841,10 +847,25 @@ __global__ void __launch_bounds__(512) few_down_kernel(FfnI8Args a, const bf16_t
 
 // Codes' rows in the workspace: whole pairs of K tiles.
 static int64_t padded(int64_t k) { return (k + 255) / 256 * 256; }
+// The first launch of a decode batch: `lists` blocks make the routing lists, the
+// others the codes of four rows each.
+__global__ void __launch_bounds__(1024) ffn_begin_kernel(FfnI8Args a, int lists, MoeLists l, int32_t* pos_of, int32_t* row_of,
+                                                         int8_t* __restrict__ q, int64_t ldq, float* __restrict__ q_scale) {
+  __shared__ uint32_t red[4][4];
+  if ((int)blockIdx.x < lists) {
+    moe_offsets_block(blockIdx.x, lists, a.ids, a.n_rows * a.k, a.E, a.k, l, pos_of, row_of);
+    return;
+  }
+  const int w = threadIdx.x >> 8;
+  // rows past the last repeat it: every thread meets the barrier, and writes the same
+  const int64_t r = min((int)(blockIdx.x - lists) * 4 + w, a.n_rows - 1);
+  quantize_row<true, true, 4>(a.x, r, threadIdx.x & 255, red[w], a.d, a.d, q, ldq, q_scale);
+}
+
 // Workspace of the expert layer, in this order, each part 256-byte aligned.
 struct FfnWork {
   int8_t *q, *hq;
-  float *q_scale, *pos_scale, *h_scale;
+  float *q_scale, *h_scale;
   int32_t *counts, *offsets, *mtiles, *n_mtiles, *mtiles_dn, *n_mtiles_dn, *blk, *pos_of, *row_of;
   bf16_t *h, *y;
 };
@@ -859,7 +880,6 @@ static size_t ffn_layout(int64_t rows, int d, int E, int k, int Fe, char* base, 
   FfnWork t;
   t.q = (int8_t*)part((size_t)rows * padded(d));
   t.q_scale = (float*)part((size_t)rows * 4);
-  t.pos_scale = (float*)part(pairs * 4);
   t.counts = (int32_t*)part((size_t)E * 4);
   t.offsets = (int32_t*)part((size_t)E * 4);
   t.mtiles = (int32_t*)part((pairs / kI8TileRowsMin + E) * 4);
@@ -904,18 +924,20 @@ hipError_t launch_moe_ffn_i8(const FfnI8Args& a, hipStream_t st) {
     else hipLaunchKernelGGL(few_down_kernel<EPI_BF16>, grid, dim3(512), lds, st, a, f.h);
     return hipGetLastError();
   }
-  hipError_t e = launch_quantize_rows(a.x, a.n_rows, a.d, a.d, true, f.q, padded(a.d), f.q_scale, st);
-  if (e != hipSuccess) return e;
-  MoeListArgs l{};
-  l.topk_id = a.ids; l.n_pairs = n_pairs; l.E = a.E; l.k = a.k;
-  l.counts = f.counts; l.offsets = f.offsets;
-  l.mtiles = f.mtiles; l.n_mtiles = f.n_mtiles; l.mtiles_dn = f.mtiles_dn; l.n_mtiles_dn = f.n_mtiles_dn;
   const int tile = grouped_i8_rows(n_pairs, a.E);
-  l.tile_rows = l.tile_rows_dn = tile;
-  l.blk = f.blk; l.pos_of = f.pos_of; l.row_of = f.row_of;
-  l.row_scale = f.q_scale; l.pos_scale = f.pos_scale;
-  if ((e = launch_moe_lists(l, st)) != hipSuccess) return e;
-  const I8Call gu{f.q, f.pos_scale, a.w_gu, a.s_gu, f.h, n_pairs, 2 * a.Fe, a.d, (int)padded(a.d), a.Fe, nullptr};
+  hipError_t e;
+  if (n_pairs <= kMoeOneBlockPairs) {
+    const MoeLists l{f.counts, f.offsets, f.mtiles, f.n_mtiles, f.mtiles_dn, f.n_mtiles_dn, nullptr, tile, tile};
+    const int lists = moe_place_blocks(n_pairs);
+    hipLaunchKernelGGL(ffn_begin_kernel, dim3(lists + (a.n_rows + 3) / 4), dim3(1024), 0, st, a, lists, l, f.pos_of, f.row_of,
+                       f.q, padded(a.d), f.q_scale);
+  } else {
+    if ((e = launch_quantize_rows(a.x, a.n_rows, a.d, a.d, true, f.q, padded(a.d), f.q_scale, st)) != hipSuccess) return e;
+    const MoeListArgs l{a.ids, n_pairs, a.E, a.k, f.counts, f.offsets, f.mtiles, f.n_mtiles, f.mtiles_dn, f.n_mtiles_dn,
+                        tile, tile, nullptr, f.blk, f.pos_of, f.row_of};
+    if ((e = launch_moe_lists(l, st)) != hipSuccess) return e;
+  }
+  const I8Call gu{f.q, f.q_scale, a.w_gu, a.s_gu, f.h, n_pairs, 2 * a.Fe, a.d, (int)padded(a.d), a.Fe, nullptr};
   if ((e = grouped_i8<EPI_SWIGLU>(tile, a.E, gu, {f.offsets, f.counts, f.mtiles, f.n_mtiles, f.row_of}, st)) != hipSuccess)
     return e;
   if ((e = launch_quantize_rows(f.h, n_pairs, a.Fe, a.Fe, true, f.hq, padded(a.Fe), f.h_scale, st)) != hipSuccess) return e;

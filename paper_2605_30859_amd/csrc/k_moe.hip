@@ -20,6 +20,7 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "moe_lists.h"
 
 namespace darts {
 
@@ -157,47 +158,11 @@ __global__ void __launch_bounds__(256) moe_topk_kernel(const float* __restrict__
   }
 }
 
-// Lists of a routing: per-expert counts and their exclusive scan, and the
-// non-empty expert row tiles (e << 16 | tile) of either projection.
-struct MoeLists {
-  int32_t *counts, *offsets, *mtiles, *n_mtiles, *mtiles2, *n_mtiles2, *touched_out;
-  int tile_rows, tile_rows2;
-};
-// The lists from thread e's count v of expert e (0 for e >= E), by one block of
-// 1024 threads; returns the expert's offset.  write: the same in the whole block.
-__device__ __forceinline__ int moe_lists(const MoeLists& l, int v, int E, int32_t* sh, bool write = true) {
-  const int tid = threadIdx.x;
-  int total;
-  const int ex = block_excl_scan1024(v, sh, &total);
-  if (!write) return ex;
-  const int nt = (v + l.tile_rows - 1) / l.tile_rows;
-  int ntiles;
-  const int tex = block_excl_scan1024(nt, sh, &ntiles);
-  if (tid < E) {
-    l.counts[tid] = v;
-    l.offsets[tid] = ex;
-    for (int j = 0; j < nt; ++j) l.mtiles[tex + j] = (tid << 16) | j;
-  }
-  if (tid == 0) *l.n_mtiles = ntiles;
-  // the second list (another row tile for the other projection)
-  const int nt2 = (v + l.tile_rows2 - 1) / l.tile_rows2;
-  int ntiles2;
-  const int tex2 = block_excl_scan1024(nt2, sh, &ntiles2);
-  if (tid < E)
-    for (int j = 0; j < nt2; ++j) l.mtiles2[tex2 + j] = (tid << 16) | j;
-  if (tid == 0) *l.n_mtiles2 = ntiles2;
-  if (l.touched_out) {
-    const int nz = __syncthreads_count(v > 0);
-    if (tid == 0) *l.touched_out = nz;
-  }
-  return ex;
-}
 // Positions of pairs [beg, end): pair i (row i / k) takes the next free slot of
 // its expert's segment (cursor[e], in LDS), pos_of and its inverse row_of.
 __device__ __forceinline__ void moe_place(const int32_t* __restrict__ topk_id, int beg, int end, int E, int k,
                                           int32_t* cursor, int32_t* __restrict__ pos_of,
-                                          int32_t* __restrict__ row_of, const float* __restrict__ row_scale,
-                                          float* __restrict__ pos_scale) {
+                                          int32_t* __restrict__ row_of) {
   for (int i = beg + (int)threadIdx.x; i < end; i += 1024) {
     const int e = topk_id[i];
     if (e < 0 || e >= E) {
@@ -207,61 +172,13 @@ __device__ __forceinline__ void moe_place(const int32_t* __restrict__ topk_id, i
     const int p = atomicAdd(&cursor[e], 1);
     pos_of[i] = p;
     row_of[p] = i / k;
-    if (pos_scale) pos_scale[p] = row_scale[i / k];
   }
 }
 
-// Decode batches: one launch, counts by an LDS histogram of the n_pairs routed
-// (row, slot) pairs.  A thread keeps its pairs' experts and their places among the
-// expert's pairs (what the histogram's adds return) in registers.  Every block
-// counts all pairs, the first writes the lists, and each places the pairs of its
-// own share of the experts: the stores to 64 different lines per instruction are
-// what placing costs (7808 pairs 18 us in one block that counted twice, 15 in one
-// that counted once).
-constexpr int kMoePlaceBlocks = 16, kMoePlaceAlone = 512;   // blocks, from so many pairs on
-constexpr int kMoeOneBlockPairs = 16384;
 __global__ void __launch_bounds__(1024) moe_offsets_kernel(const int32_t* __restrict__ topk_id, int n_pairs, int E,
                                                            int k, MoeLists lists, int32_t* __restrict__ pos_of,
-                                                           int32_t* __restrict__ row_of,
-                                                           const float* __restrict__ row_scale,
-                                                           float* __restrict__ pos_scale) {
-  constexpr int N = kMoeOneBlockPairs / 1024;
-  __shared__ int32_t hist[1024];
-  __shared__ int32_t sh[32];
-  const int tid = threadIdx.x;
-  int e[N], at[N];
-#pragma unroll
-  for (int u = 0; u < N; ++u) {
-    e[u] = -1;
-    if (1024 * u < n_pairs && tid + 1024 * u < n_pairs) e[u] = topk_id[tid + 1024 * u];
-  }
-  hist[tid] = 0;
-  __syncthreads();
-#pragma unroll
-  for (int u = 0; u < N; ++u) {
-    if (1024 * u >= n_pairs) break;
-    at[u] = -1;
-    if (e[u] >= 0 && e[u] < E) at[u] = atomicAdd(&hist[e[u]], 1);
-  }
-  __syncthreads();
-  const int ex = moe_lists(lists, tid < E ? hist[tid] : 0, E, sh, blockIdx.x == 0);
-  hist[tid] = tid < E ? ex : 0;          // the experts' first positions
-  __syncthreads();
-  const int lo = (int)(blockIdx.x * E / gridDim.x), hi = (int)((blockIdx.x + 1) * E / gridDim.x);
-#pragma unroll
-  for (int u = 0; u < N; ++u) {
-    const int i = tid + 1024 * u;
-    if (1024 * u >= n_pairs) break;
-    if (i >= n_pairs) continue;
-    if (at[u] < 0) {
-      if (blockIdx.x == 0) pos_of[i] = -1;
-    } else if (e[u] >= lo && e[u] < hi) {
-      const int p = hist[e[u]] + at[u];
-      row_of[p] = i / k;
-      if (pos_scale) pos_scale[p] = row_scale[i / k];
-      pos_of[i] = p;
-    }
-  }
+                                                           int32_t* __restrict__ row_of) {
+  moe_offsets_block(blockIdx.x, gridDim.x, topk_id, n_pairs, E, k, lists, pos_of, row_of);
 }
 
 // Large batches (the prefill): the pairs go to kMoeBlocks blocks, which count
@@ -303,15 +220,12 @@ __global__ void __launch_bounds__(1024) moe_scan_kernel(int E, MoeLists lists, i
 }
 __global__ void __launch_bounds__(1024) moe_place_kernel(const int32_t* __restrict__ topk_id, int n_pairs, int E,
                                                          int k, const int32_t* __restrict__ blk,
-                                                         int32_t* __restrict__ pos_of, int32_t* __restrict__ row_of,
-                                                         const float* __restrict__ row_scale,
-                                                         float* __restrict__ pos_scale) {
+                                                         int32_t* __restrict__ pos_of, int32_t* __restrict__ row_of) {
   __shared__ int32_t cursor[1024];
   const int tid = threadIdx.x, b = blockIdx.x;
   cursor[tid] = tid < E ? blk[b * E + tid] : 0;
   __syncthreads();
-  moe_place(topk_id, moe_block_begin(b, n_pairs), moe_block_begin(b + 1, n_pairs), E, k, cursor, pos_of, row_of,
-            row_scale, pos_scale);
+  moe_place(topk_id, moe_block_begin(b, n_pairs), moe_block_begin(b + 1, n_pairs), E, k, cursor, pos_of, row_of);
 }
 
 // x[r] += sum_j w[r][j] * y[pos(r, j)]   (slot order, y in bf16, the sum in
@@ -408,13 +322,13 @@ hipError_t launch_moe_lists(const MoeListArgs& a, hipStream_t st) {
   const MoeLists lists{a.counts, a.offsets, a.mtiles, a.n_mtiles, a.mtiles_dn, a.n_mtiles_dn, a.touched_out,
                        a.tile_rows, a.tile_rows_dn};
   if (a.n_pairs <= kMoeOneBlockPairs) {
-    hipLaunchKernelGGL(moe_offsets_kernel, dim3(a.n_pairs < kMoePlaceAlone ? 1 : kMoePlaceBlocks), dim3(1024), 0, st, a.topk_id, a.n_pairs, a.E, a.k, lists, a.pos_of,
-                       a.row_of, a.row_scale, a.pos_scale);
+    hipLaunchKernelGGL(moe_offsets_kernel, dim3(moe_place_blocks(a.n_pairs)), dim3(1024), 0, st, a.topk_id, a.n_pairs, a.E,
+                       a.k, lists, a.pos_of, a.row_of);
   } else {
     hipLaunchKernelGGL(moe_count_kernel, dim3(kMoeBlocks), dim3(1024), 0, st, a.topk_id, a.n_pairs, a.E, a.blk);
     hipLaunchKernelGGL(moe_scan_kernel, dim3(1), dim3(1024), 0, st, a.E, lists, a.blk);
     hipLaunchKernelGGL(moe_place_kernel, dim3(kMoeBlocks), dim3(1024), 0, st, a.topk_id, a.n_pairs, a.E, a.k, a.blk,
-                       a.pos_of, a.row_of, a.row_scale, a.pos_scale);
+                       a.pos_of, a.row_of);
   }
   return hipGetLastError();
 }
@@ -454,7 +368,7 @@ hipError_t launch_moe_ffn(const MoeArgs& a, hipStream_t st, bool* normed) {
 #undef DARTS_TOPK
   const MoeListArgs lists{a.topk_id, a.n_rows * a.k, a.E, a.k, a.counts, a.offsets, a.mtiles, a.n_mtiles, a.mtiles_dn,
                           a.n_mtiles_dn, plan_gu.tile_rows, plan_dn.tile_rows, a.touched_out, a.blk, a.pos_of,
-                          a.row_of, nullptr, nullptr};
+                          a.row_of};
   if ((e = launch_moe_lists(lists, st)) != hipSuccess) return e;
   const int Fe = a.Fe, d = a.d;
   // gate/up: N = 2*Fe, K = d (SwiGLU into h_perm), A rows gathered from xn;

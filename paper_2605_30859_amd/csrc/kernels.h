@@ -281,7 +281,6 @@ struct MoeListArgs {
   int tile_rows, tile_rows_dn;
   int32_t* touched_out;
   int32_t *blk, *pos_of, *row_of;
-  const float* row_scale; float* pos_scale;   // pos_scale[p] = row_scale[row_of[p]] (NULL: none)
 };
 hipError_t launch_moe_lists(const MoeListArgs& a, hipStream_t st);
 
