@@ -628,7 +628,7 @@ int darts_moe_route(const void* d_logits, int64_t ld, int32_t n_rows, int32_t n_
  * scale NaN and codes 0 (its products are NaN).
  *   d_x     rows of cols elements (bf16 or f32), ldx elements apart
  *   d_q     [rows][cols] int8 out,  d_scale [rows] float32 out
- * DARTS_EINVAL for rows < 0, cols < 1 or ldx < cols.                       */
+ * DARTS_EINVAL for rows < 0, cols < 1, cols > 2^30 or ldx < cols.          */
 int darts_quantize_rows(const void* d_x, int64_t ldx, int32_t rows, int32_t cols, int32_t dtype, int8_t* d_q,
                         float* d_scale, void* stream);
 
@@ -638,9 +638,9 @@ int darts_quantize_rows(const void* d_x, int64_t ldx, int32_t rows, int32_t cols
  * and the epilogues of darts_gemm: 0 float32 stored, 1 bf16 stored, 2 added to a
  * float32 d_c, 3 SwiGLU (W rows and their scales interleaved in groups of 16;
  * d_c [M][N/2] bf16).
- *   d_a [M][K], d_w [N][K] codes, 16-byte aligned; K and N multiples of 16 (N of
- *   32 for SwiGLU), K <= 131072 (so that the sum fits), and fewer than 2^24 tiles
- *   of 64 x 64 results.  d_workspace must hold
+ *   d_a [M][K], d_w [N][K] codes, 16-byte aligned as d_c is; K and N multiples of
+ *   16 (N of 32 for SwiGLU), K <= 131072 (so that the sum fits), and fewer than 2^24
+ *   tiles of 64 x 64 results.  d_workspace must hold
  *   darts_gemm_i8_workspace_bytes(M, N, K) bytes, 16-byte aligned.         */
 size_t darts_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K);
 int darts_gemm_i8(const int8_t* d_a, const float* d_a_scale, const int8_t* d_w, const float* d_w_scale,
@@ -662,7 +662,8 @@ int darts_gemm_i8(const int8_t* d_a, const float* d_a_scale, const int8_t* d_w, 
  *   d_out      [n_rows][d_model]: epilogue 1 bf16 stored, 2 added to float32
  *   d_workspace darts_moe_ffn_i8_workspace_bytes(...) bytes, 256-byte aligned
  * Codes, d_x and d_out are 16-byte aligned.  d_model and expert_ffn are multiples of 16
- * up to 131072, n_experts <= 1024, top_k <= 64, n_rows * top_k <= 4194240.
+ * up to 131072, n_experts <= 1024, top_k <= 64, n_rows * top_k <= 4194240, and
+ * n_rows times d_model, rounded up to a multiple of 256, is at most 2^32 - 256.
  * Calls that overlap in time need workspaces of their own, captured graphs too. */
 size_t darts_moe_ffn_i8_workspace_bytes(int32_t n_rows, int32_t d_model, int32_t n_experts, int32_t top_k,
                                         int32_t expert_ffn);

@@ -1400,7 +1400,7 @@ int darts_moe_route(const void* d_logits, int64_t ld, int32_t n_rows, int32_t n_
 
 int darts_quantize_rows(const void* d_x, int64_t ldx, int32_t rows, int32_t cols, int32_t dtype, int8_t* d_q,
                         float* d_scale, void* stream) {
-  if (rows < 0 || cols < 1 || ldx < cols) return DARTS_EINVAL;
+  if (rows < 0 || cols < 1 || cols > (1 << 30) || ldx < cols) return DARTS_EINVAL;
   if (dtype != DARTS_F32 && dtype != DARTS_BF16) return DARTS_EINVAL;
   if (rows == 0) return DARTS_OK;
   if (!d_x || !d_q || !d_scale) return DARTS_EINVAL;
@@ -1410,6 +1410,7 @@ int darts_quantize_rows(const void* d_x, int64_t ldx, int32_t rows, int32_t cols
 
 constexpr int kI8MaxK = 131072;   // 127 * 127 * 131072 < 2^31
 constexpr int64_t kI8MaxPairs = (int64_t)65535 * 64;   // an expert's row tiles fit 16 bits
+constexpr int64_t kI8MaxCodes = ((int64_t)1 << 32) - 256;   // gathered rows are at 32-bit offsets from the first
 
 size_t darts_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K) {
   if (M < 1 || N < 1 || K < 1) return 0;
@@ -1424,7 +1425,7 @@ int darts_gemm_i8(const int8_t* d_a, const float* d_a_scale, const int8_t* d_w, 
   if (((int64_t)M + 63) / 64 * (((int64_t)N + 63) / 64) >= (1 << 24)) return DARTS_EINVAL;   // too many tiles for a launch
   if (M == 0) return DARTS_OK;
   if (!d_a || !d_a_scale || !d_w || !d_w_scale || !d_c) return DARTS_EINVAL;
-  if (!aligned16(d_a) || !aligned16(d_w) || !aligned16(d_workspace)) return DARTS_EINVAL;
+  if (!aligned16(d_a) || !aligned16(d_w) || !aligned16(d_c) || !aligned16(d_workspace)) return DARTS_EINVAL;
   const size_t need = gemm_i8_workspace_bytes(M, N, K);
   if (need > workspace_bytes || (need && !d_workspace)) return DARTS_EINVAL;
   hipError_t e = launch_gemm_i8(d_a, d_a_scale, d_w, d_w_scale, d_c, M, N, K, epilogue, d_workspace, workspace_bytes,
@@ -1434,7 +1435,8 @@ int darts_gemm_i8(const int8_t* d_a, const float* d_a_scale, const int8_t* d_w, 
 
 static bool ffn_i8_sizes(int32_t n_rows, int32_t d, int32_t E, int32_t k, int32_t Fe) {
   return n_rows >= 0 && d >= 16 && d % 16 == 0 && d <= kI8MaxK && Fe >= 16 && Fe % 16 == 0 && Fe <= kI8MaxK &&
-         E >= 1 && E <= 1024 && k >= 1 && k <= 64 && (int64_t)n_rows * k <= kI8MaxPairs;
+         E >= 1 && E <= 1024 && k >= 1 && k <= 64 && (int64_t)n_rows * k <= kI8MaxPairs &&
+         (int64_t)n_rows * ((d + 255) / 256 * 256) <= kI8MaxCodes;
 }
 
 size_t darts_moe_ffn_i8_workspace_bytes(int32_t n_rows, int32_t d_model, int32_t n_experts, int32_t top_k,

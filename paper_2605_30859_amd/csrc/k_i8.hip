@@ -67,8 +67,9 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 }
 
 // WPR wavefronts per row, blocks of four.  VEC: rows of whole 16-byte pieces, codes
-// ldq apart with zeros between them (else ldq is cols); the first kQuantKeep pieces of a lane stay in registers between the two passes, so
-// rows of up to 64 * WPR * 32 elements are read once.
+// ldq apart with zeros between them (else ldq is cols); the first kQuantKeep pieces
+// of a lane stay in registers between the two passes, so rows of up to
+// 64 * WPR * 32 elements are read once.
 constexpr int kQuantKeep = 4;
 template <bool BF16, bool VEC, int WPR>
 __device__ __forceinline__ void quantize_row(const void* __restrict__ x, int64_t r, int t, uint32_t* red, int cols, int64_t ldx,
@@ -363,7 +364,7 @@ static bool set_i8_plan(I8Plan& p, int kind, int S, int M, int N, int K) {
   p.mt = p.nt = 0;
   p.k_chunk = K2;
   p.pad = false;
-  if (kind < 0) return M <= 32 && (S == 4 || S == 8);
+  if (kind < 0) return M <= 32 && (S == 4 || S == 8) && (int64_t)N * S < ((int64_t)1 << 29);   // 512 N S / 128 threads
   const I8Tiles& t = kI8Tiles[kind];
   p.mt = (M + t.bm - 1) / t.bm;
   p.nt = (N + t.bn - 1) / t.bn;
@@ -653,8 +654,8 @@ static hipError_t grouped_i8(int rows, int E, const I8Call& c, const I8Groups& g
 // ------------------------------------------------------------ routed experts
 // out[r] = sum_j w[r][j] * y[pos(r, j)] in slot order, fp32 sums, 8 columns per
 // thread; y is read once, non-temporal (a layer of 8000 rows 482 us, 590 with plain
-// loads; 32768 rows 1657 and 1785).  A place without an expert adds w * 0: nothing, or NaN for the weight
-// NaN of a row that the router could not read.
+// loads; 32768 rows 1657 and 1785).  A place without an expert adds w * 0: nothing,
+// or NaN for the weight NaN of a row that the router could not read.
 template <int EPI>
 __global__ void __launch_bounds__(256) combine_i8_kernel(const bf16_t* __restrict__ y, int d, int k,
                                                          const int32_t* __restrict__ pos_of,
@@ -699,7 +700,9 @@ __global__ void __launch_bounds__(256) combine_i8_kernel(const bf16_t* __restric
 // and every row of the matrix instruction's other operand is the pair's own.
 // Loads return in the order of their issue: the activations' come first, the
 // weights' are in flight while the codes are made.
-constexpr int kFewU = 2;                       // loads of 64 codes in one step (one row of 128 experts: 13.0 us, with 4 13.4, with 8 17.0)
+// Loads of 64 codes in one step (one row of 128 experts: 13.0 us, with 4 13.4, with 8
+// 17.0).
+constexpr int kFewU = 2;
 struct FewStrip {
   const int8_t* w;
   int K;

@@ -25,6 +25,8 @@
 // logits takes 3 us.  976 rows of 256 experts in 8 groups with a bias: 15 and 8 us.
 #include <math.h>
 
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 
@@ -422,14 +424,21 @@ static void route_go(const RouteArgs& a, hipStream_t st) {
 #undef DARTS_ROUTE
 }
 
-hipError_t launch_route(const RouteArgs& a, hipStream_t st) {
-  if (a.n_rows <= 0) return hipSuccess;
-  if (a.n_experts > 1024 || a.top_k > 64 || a.n_groups > 64) return hipErrorInvalidValue;
-  if (a.n_experts <= 64 && a.top_k < 16) route_go<16, 4>(a, st);
-  else if (a.n_experts <= 128 && a.top_k < 16) route_go<16, 8>(a, st);
-  else if (a.n_experts <= 256 && a.top_k < 32) route_go<32, 8>(a, st);
-  else if (a.n_experts <= 512) route_go<64, 8>(a, st);
-  else route_go<64, 16>(a, st);
+hipError_t launch_route(const RouteArgs& all, hipStream_t st) {
+  if (all.n_experts > 1024 || all.top_k > 64 || all.n_groups > 64) return hipErrorInvalidValue;
+  constexpr int most = 1 << 24;        // rows of a launch: up to 64 threads each, fewer than 2^32 in all
+  for (int64_t r = 0; r < all.n_rows; r += most) {
+    RouteArgs a = all;
+    a.logits = (const char*)all.logits + r * all.ld * (all.bf16 ? 2 : 4);
+    a.ids += r * all.top_k;
+    a.weights += r * all.top_k;
+    a.n_rows = (int)std::min<int64_t>(all.n_rows - r, most);
+    if (a.n_experts <= 64 && a.top_k < 16) route_go<16, 4>(a, st);
+    else if (a.n_experts <= 128 && a.top_k < 16) route_go<16, 8>(a, st);
+    else if (a.n_experts <= 256 && a.top_k < 32) route_go<32, 8>(a, st);
+    else if (a.n_experts <= 512) route_go<64, 8>(a, st);
+    else route_go<64, 16>(a, st);
+  }
   return hipGetLastError();
 }
 

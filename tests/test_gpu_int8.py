@@ -204,6 +204,25 @@ def test_results_beyond_32_bit_offsets():
     assert bool(((out[rows].double() - ref).abs() <= 3.01 * 2.0 ** -24 * ref.abs()).all())
 
 
+def test_more_channels_than_a_launch_of_strips_has():
+    """One row and 2^28 + 32 channels, 4 GB of codes."""
+    N, K = (1 << 28) + 32, 16
+    g = _gen(1, 1, K)
+    a = torch.randint(-127, 128, (1, K), dtype=torch.int8, device=DEV, generator=g)
+    w = torch.randint(-127, 128, (N, K), dtype=torch.int8, device=DEV, generator=g)
+    sa, sw = torch.full((1,), 0.5, device=DEV), torch.full((N,), 2.0, device=DEV)
+    out = torch.full((N + 16,), 3.0, device=DEV)
+    _b().darts_gemm_i8(a, sa, w, sw, out, 1, N, K, 0, None)
+    # sums below 2^24, and scales of powers of two: exact in float32
+    for at in range(0, N, 1 << 24):
+        rows = w[at:at + (1 << 24)]
+        ref = torch.zeros(rows.shape[0], device=DEV)
+        for j in range(K):
+            ref += rows[:, j].float() * a[0, j].float()
+        assert torch.equal(out[at:at + rows.shape[0]], ref)
+    assert bool((out[N:] == 3.0).all())
+
+
 # -------------------------------------------------------------------- experts
 def _layer(E, d, F, seed=0):
     g = _gen(E, d, F, seed)

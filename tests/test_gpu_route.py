@@ -159,6 +159,17 @@ def test_many_rows():
     assert (np.abs(w - ew) <= ew * (2.0 ** -24 * (1 + 1e-6))).all()
 
 
+@pytest.mark.parametrize("E,k", [(4, 2), (4, 4)])
+def test_more_rows_than_one_launch_has(E, k):
+    """2^24 + 5 rows, copies of 64: all as the first."""
+    l = _logits(64, E)
+    l = l.repeat((1 << 18) + 1, 1)[:(1 << 24) + 5].contiguous()
+    ids, w = _call(l, k)
+    eid, ew = _call(l[:64].contiguous(), k)
+    n = len(ids)
+    assert (ids == np.tile(eid, (n // 64 + 1, 1))[:n]).all() and (w == np.tile(ew, (n // 64 + 1, 1))[:n]).all()
+
+
 def test_other_stream_and_graph_replays():
     B = _b()
     l = _logits(300, 256)

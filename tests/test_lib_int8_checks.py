@@ -79,3 +79,14 @@ def test_binding_wants_adjacent_elements():
         B.darts_quantize_rows(x, B.DARTS_F32, None, None)
     with pytest.raises(ValueError):
         B.darts_moe_route(x, B.DARTS_F32, x, x)
+
+
+def test_refusals_of_sizes_past_the_kernels_offsets(lib):
+    # a row of codes longer than 2^30; results that are not 16-byte aligned; gathered
+    # rows beyond 32-bit offsets
+    assert lib.darts_quantize_rows(D, 1 << 31, 1, (1 << 30) + 1, B.DARTS_F32, D, D, N) == EINVAL
+    assert lib.darts_gemm_i8(D, D, D, D, ODD, 4, 64, 64, 0, D, 1 << 40, N) == EINVAL
+    for rows, d in ((1 << 19, 8192), ((1 << 24) // 16, 4096), (32768, 131072), (4194240, 1040)):
+        assert lib.darts_moe_ffn_i8_workspace_bytes(rows, d, 8, 1, 32) == 0, (rows, d)
+        assert lib.darts_moe_ffn_i8(D, D, D, rows, d, 8, 1, 32, D, D, D, D, D, 1, D, 1 << 50, N) == EINVAL, (rows, d)
+    assert lib.darts_moe_ffn_i8_workspace_bytes((1 << 19) - 1, 8192, 8, 1, 32) > 0
