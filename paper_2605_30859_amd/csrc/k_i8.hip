@@ -66,7 +66,7 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
   return v;
 }
 
-// WPR wavefronts per row, blocks of four.  VEC: rows of whole 16-byte pieces, codes
+// WPR wavefronts per row, in blocks of four or sixteen.  VEC: rows of whole 16-byte pieces, codes
 // ldq apart with zeros between them (else ldq is cols); the first kQuantKeep pieces
 // of a lane stay in registers between the two passes, so rows of up to
 // 64 * WPR * 32 elements are read once.
@@ -97,10 +97,11 @@ __device__ __forceinline__ void quantize_row(const void* __restrict__ x, int64_t
     for (int c = t; c < cols; c += T) top = max(top, __float_as_uint(load_x<BF16>(x, r * ldx + c)) & 0x7fffffffu);
   }
   top = wave_max_u32(top);
-  if constexpr (WPR == 4) {                            // in a block, every row at once
+  if constexpr (WPR > 1) {                             // in a block, every row at once
     if ((t & 63) == 0) red[t >> 6] = top;
     __syncthreads();
-    top = max(max(red[0], red[1]), max(red[2], red[3]));
+#pragma unroll
+    for (int i = 0; i < WPR; ++i) top = max(top, red[i]);
   }
   float up, sc;
   row_scale(top, up, sc);
@@ -131,31 +132,33 @@ __device__ __forceinline__ void quantize_row(const void* __restrict__ x, int64_t
 }
 
 template <bool BF16, bool VEC, int WPR>
-__global__ void __launch_bounds__(256) quantize_rows_kernel(const void* __restrict__ x, int64_t rows, int cols, int64_t ldx,
-                                                            int8_t* __restrict__ q, int64_t ldq,
-                                                            float* __restrict__ scale) {
-  __shared__ uint32_t red[4];
-  const int64_t r = (int64_t)blockIdx.x * (4 / WPR) + threadIdx.x / (64 * WPR);
-  if (r >= rows) return;                               // the whole wavefront; with WPR 4 no block has any
+__global__ void __launch_bounds__(std::max(256, 64 * WPR))
+    quantize_rows_kernel(const void* __restrict__ x, int64_t rows, int cols, int64_t ldx, int8_t* __restrict__ q, int64_t ldq,
+                         float* __restrict__ scale) {
+  __shared__ uint32_t red[WPR];
+  const int64_t r = WPR == 1 ? (int64_t)blockIdx.x * 4 + threadIdx.x / 64 : blockIdx.x;
+  if (WPR == 1 && r >= rows) return;
   quantize_row<BF16, VEC, WPR>(x, r, threadIdx.x % (64 * WPR), red, cols, ldx, q, ldq, scale);
 }
 
 template <bool BF16, bool VEC>
 static hipError_t quantize_go(const void* x, int64_t rows, int cols, int64_t ldx, int8_t* q, int64_t ldq, float* scale,
                               hipStream_t st) {
-  // a wavefront per row where it holds the row, and there are rows for every CU
-  const int wpr = cols <= 64 * 8 * kQuantKeep && rows >= 2048 ? 1 : 4;
-  const int64_t most = (int64_t)(1 << 22) * (4 / wpr);       // rows per launch
+  // A wavefront per row where it holds the row, and there are rows for every CU; four
+  // up to what they hold, and 16 beyond.  Four and 16, bf16, us: 45 rows of 8192 2.8 /
+  // 2.8, of 12288 3.5 / 3.0, of 24576 5.9 / 3.7; 7808 rows 30 / 38, 49 / 46, 132 / 99.
+  constexpr int hold = 64 * 8 * kQuantKeep;
+  const int wpr = cols <= hold && rows >= 2048 ? 1 : cols <= 4 * hold ? 4 : 16;
+  const int64_t most = (int64_t)1 << 21;               // rows per launch
   for (int64_t r = 0; r < rows; r += most) {
     const int64_t n = std::min(rows - r, most);
-    const dim3 grid((unsigned)((n * wpr + 3) / 4));
     const char* xr = (const char*)x + r * ldx * (BF16 ? 2 : 4);
-    if (wpr == 1)
-      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 1>), grid, dim3(256), 0, st, xr, n, cols, ldx, q + r * ldq,
-                         ldq, scale + r);
-    else
-      hipLaunchKernelGGL((quantize_rows_kernel<BF16, VEC, 4>), grid, dim3(256), 0, st, xr, n, cols, ldx, q + r * ldq,
-                         ldq, scale + r);
+    auto go = [&](auto kern, unsigned blocks, int threads) {
+      hipLaunchKernelGGL(kern, dim3(blocks), dim3(threads), 0, st, xr, n, cols, ldx, q + r * ldq, ldq, scale + r);
+    };
+    if (wpr == 1) go(quantize_rows_kernel<BF16, VEC, 1>, (unsigned)((n + 3) / 4), 256);
+    else if (wpr == 4) go(quantize_rows_kernel<BF16, VEC, 4>, (unsigned)n, 256);
+    else go(quantize_rows_kernel<BF16, VEC, 16>, (unsigned)n, 1024);
   }
   return hipGetLastError();
 }
