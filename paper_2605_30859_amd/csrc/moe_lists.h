@@ -46,7 +46,7 @@ __device__ __forceinline__ int moe_lists(const MoeLists& l, int v, int E, int32_
 // counts all pairs, the first writes the lists, and each places the pairs of its
 // own share of the experts: the stores to 64 different lines per instruction are
 // what placing costs (7808 pairs 18 us in one block that counted twice, 15 in one
-// that counted once).
+// that counted once, 9.8 so).
 constexpr int kMoePlaceBlocks = 16, kMoePlaceAlone = 512;   // blocks, from so many pairs on
 constexpr int kMoeOneBlockPairs = 16384;
 // Block `blk` of `blks` blocks of 1024 threads.
