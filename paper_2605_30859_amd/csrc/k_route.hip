@@ -14,11 +14,11 @@
 // maximum over the row of
 //  * the logits themselves where there is neither bias nor group: scores rise with
 //    them, and equal logits have equal scores;
-//  * t in float32 otherwise, off by less than 2^-20 (1 + |t|).  One more than k are
-//    taken, and these ordered by their 64-bit t.
-// Where a value left out is so near to the last one taken (kNearScore; kNearLogit
-// between any two logits) that the definition might see them otherwise, or scores
-// saturate, the row is done again by the definition, by the whole wavefront.
+//  * t in float32 otherwise, off by less than 2^-20 (1 + |t|), with sigmoids 2^-22.
+//    One more than k are taken, and these ordered by their 64-bit t.
+// Where a value left out is so near to the last one taken (kNearSoftmax, kNearSigmoid;
+// kNearLogit between any two logits) that the definition might see them otherwise, or
+// scores saturate, the row is done again by the definition, by the whole wavefront.
 //
 // Bound by instructions.  32768 rows of 128 experts: 51 us by the definition alone
 // (a wavefront per row, ranks by comparing every pair), 13 us so; reading the
@@ -37,7 +37,10 @@ constexpr int kRouteWaves = 4;       // wavefronts per block
 // 2^-26 at least 1 + 4e-15, which 64 bits tell apart.
 constexpr float kNearLogit = 1.490116119384765625e-08f;   // 2^-26
 constexpr float kSigmoidTop = 15.f, kScoreLow = -700.f;
-constexpr float kNearScore = 3.814697265625e-06f;   // 2^-18, relative to 1 + |t|
+// Relative to 1 + |t|, for groups to 1 and their experts' |t|: four errors of softmax
+// scores (the exponentials', and their sum's); of sigmoids 1.25 2^-23 + 2^-24 |t| each
+// and the sums' roundings.  A row done again costs a small call 6 us.
+constexpr float kNearSoftmax = 3.814697265625e-06f, kNearSigmoid = 9.5367431640625e-07f;   // 2^-18, 2^-20
 
 __device__ __forceinline__ double wave_sum_f64(double v) {
 #pragma unroll
@@ -246,7 +249,7 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a) {
   } else {
     if (a.sigmoid) {
 #pragma unroll
-      for (int j = 0; j < NPL; ++j) t[j] = 1.0f / (1.0f + __expf(-l[j]));
+      for (int j = 0; j < NPL; ++j) t[j] = __fdiv_rn(1.0f, 1.0f + expf(-l[j]));
     } else {
       const float base = mx == -INFINITY ? 0.f : mx;
       float sum = 0.f;
@@ -275,10 +278,11 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a) {
   }
   const bool bad = row_reduce<LPR>(odd, max_f) > 0.f;
   bool near = false;
+  const float near_by = a.sigmoid ? kNearSigmoid : kNearSoftmax;
   auto too_near = [&](float hi, float lo) {           // hi >= lo, neighbours in the order; lo may be -inf
     const float gap = hi - lo;
     if (MODE == ROUTE_LOGITS) return gap > 0.f && gap < kNearLogit;
-    return gap < kNearScore * (1.0f + fmaxf(fabsf(hi), fabsf(lo)));
+    return gap < near_by * (1.0f + fmaxf(fabsf(hi), fabsf(lo)));
   };
   if constexpr (MODE == ROUTE_GROUPS) {
     // the two best of each group's lanes, then the groups' values against each other
@@ -294,7 +298,10 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a) {
       v1 = fmaxf(fminf(v0, u0), fmaxf(v1, u1));
       v0 = fmaxf(v0, u0);
     }
-    const float v = a.group_best == 2 && v1 > -INFINITY ? v0 + v1 : v0;
+    const bool two = a.group_best == 2 && v1 > -INFINITY;
+    const float v = two ? v0 + v1 : v0;
+    // experts of opposite signs may have a small sum: its error goes by their sizes
+    const float size = v0 > -INFINITY ? fabsf(v0) + (two ? fabsf(v1) : 0.f) : 0.f;
     const int g = sub / lanes;
     int before = 0;
 #pragma unroll 4
@@ -305,7 +312,7 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a) {
     const bool in = e0 < E, stays = in && before < a.top_groups;
     const float low = row_reduce<LPR>(stays ? v : INFINITY, min_f);
     const float high = row_reduce<LPR>(in && !stays ? v : -INFINITY, max_f);
-    near = low > -INFINITY && too_near(low, high);
+    near = low > -INFINITY && low - high < near_by * (1.0f + row_reduce<LPR>(in ? size : 0.f, max_f));
 #pragma unroll
     for (int j = 0; j < NPL; ++j) t[j] = stays ? t[j] : -INFINITY;
   }

@@ -138,6 +138,16 @@ def test_large_bias(bias):
         _check(l, 8, score=score, bias=b)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("large", [10.0, 1000.0])
+def test_groups_of_large_biases_of_either_sign(score, large):
+    """Groups whose two best add up to little: float32 keeps few digits of either."""
+    bias = torch.full((32,), -3.0 * large, device=DEV)
+    bias[0::4], bias[1::4] = large, -large
+    # taken: the large ones of three groups
+    _check(_logits(20000, 32), 3, score=score, bias=bias, n_groups=8, top_groups=3, group_best=2)
+
+
 def test_strided_rows():
     wide = _logits(50, 384)
     wide[:, 60:] = float("nan")       # columns beside the logits are not read
