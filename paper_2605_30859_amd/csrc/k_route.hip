@@ -37,9 +37,10 @@ constexpr int kRouteWaves = 4;       // wavefronts per block
 // 2^-26 at least 1 + 4e-15, which 64 bits tell apart.
 constexpr float kNearLogit = 1.490116119384765625e-08f;   // 2^-26
 constexpr float kSigmoidTop = 15.f, kScoreLow = -700.f;
-// Relative to 1 + |t|, for groups to 1 and their experts' |t|: four errors of softmax
-// scores (the exponentials', and their sum's); of sigmoids 1.25 2^-23 + 2^-24 |t| each
-// and the sums' roundings.  A row done again costs a small call 6 us.
+// Relative to 1 + |t|, for a pair of groups to 1 and the mean of either's experts' |t|:
+// four errors of softmax scores (the exponentials', and their sum's); of sigmoids
+// 1.25 2^-23 + 2^-24 |t| each and the sums' roundings.  A row done again costs a small
+// call 6 to 9 us.
 constexpr float kNearSoftmax = 3.814697265625e-06f, kNearSigmoid = 9.5367431640625e-07f;   // 2^-18, 2^-20
 
 __device__ __forceinline__ double wave_sum_f64(double v) {
@@ -298,10 +299,12 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a) {
       v1 = fmaxf(fminf(v0, u0), fmaxf(v1, u1));
       v0 = fmaxf(v0, u0);
     }
+    // Half of a value, or of two experts' mean, which finite scores do not overflow.  Its
+    // error goes by its own experts' sizes (of opposite signs they may have a small sum).
     const bool two = a.group_best == 2 && v1 > -INFINITY;
-    const float v = two ? v0 + v1 : v0;
-    // experts of opposite signs may have a small sum: its error goes by their sizes
-    const float size = v0 > -INFINITY ? fabsf(v0) + (two ? fabsf(v1) : 0.f) : 0.f;
+    const float f = a.group_best == 2 ? 0.25f : 0.5f;
+    const float v = two ? f * v0 + f * v1 : f * v0;
+    const float err = v0 > -INFINITY ? 0.5f * near_by * (f + f * fabsf(v0) + (two ? f * fabsf(v1) : 0.f)) : 0.f;
     const int g = sub / lanes;
     int before = 0;
 #pragma unroll 4
@@ -310,9 +313,9 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a) {
       before += (u > v) | ((u == v) & (i < g));
     }
     const bool in = e0 < E, stays = in && before < a.top_groups;
-    const float low = row_reduce<LPR>(stays ? v : INFINITY, min_f);
-    const float high = row_reduce<LPR>(in && !stays ? v : -INFINITY, max_f);
-    near = low > -INFINITY && low - high < near_by * (1.0f + row_reduce<LPR>(in ? size : 0.f, max_f));
+    const float low = row_reduce<LPR>(stays ? v - err : INFINITY, min_f);
+    const float high = row_reduce<LPR>(in && !stays ? v + err : -INFINITY, max_f);
+    near = low > -INFINITY && low <= high;
 #pragma unroll
     for (int j = 0; j < NPL; ++j) t[j] = stays ? t[j] : -INFINITY;
   }
