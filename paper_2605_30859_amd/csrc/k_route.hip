@@ -387,7 +387,9 @@ __global__ void __launch_bounds__(64 * kRouteWaves) route_kernel(RouteArgs a) {
     for (int o = LPR / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
     v = sum > 0.0 ? v / sum : 0.0;
   }
-  if (live && place < k) {
+  // near and bad are the same in the whole row; a row that is done again is written there
+  // alone, as other lanes hold its places
+  if (live && place < k && (bad || !near)) {
     a.ids[r * k + place] = bad ? -1 : my_id;
     a.weights[r * k + place] = bad ? __uint_as_float(0x7fc00000u) : (float)(v * (double)a.factor);
   }
