@@ -652,7 +652,7 @@ int darts_gemm_i8(const int8_t* d_a, const float* d_a_scale, const int8_t* d_w, 
  *   h = bf16(silu(g) * u) with g, u the gate and up products of x's codes (as
  *   darts_quantize_rows makes them), y = bf16(the down product of h's codes),
  *   out[r] = sum_j weights[r][j] * y_j   (float32, slot order)
- * Pairs with another id add nothing (and NaN where their weight is NaN).
+ * Pairs with another id add nothing, whatever their weight, but NaN where it is NaN.
  *   d_x        [n_rows][d_model] bf16
  *   d_ids, d_weights  [n_rows][top_k] int32 and float32, as darts_moe_route
  *              writes them; an id may come twice in a row

@@ -657,8 +657,9 @@ static hipError_t grouped_i8(int rows, int E, const I8Call& c, const I8Groups& g
 // ------------------------------------------------------------ routed experts
 // out[r] = sum_j w[r][j] * y[pos(r, j)] in slot order, fp32 sums, 8 columns per
 // thread; y is read once, non-temporal (a layer of 8000 rows 482 us, 590 with plain
-// loads; 32768 rows 1657 and 1785).  A place without an expert adds w * 0: nothing,
-// or NaN for the weight NaN of a row that the router could not read.
+// loads; 32768 rows 1657 and 1785).  A place without an expert adds nothing, whatever
+// its weight, but NaN for the weight NaN of a row that the router could not read.
+__device__ __forceinline__ float weight_of(bool expert, float w) { return expert || w != w ? w : 0.f; }
 template <int EPI>
 __global__ void __launch_bounds__(256) combine_i8_kernel(const bf16_t* __restrict__ y, int d, int k,
                                                          const int32_t* __restrict__ pos_of,
@@ -676,7 +677,7 @@ __global__ void __launch_bounds__(256) combine_i8_kernel(const bf16_t* __restric
         v[j].v = (u32x4_t){0u, 0u, 0u, 0u};
         if (j0 + j < k) {
           const int p = pos_of[r * k + j0 + j];
-          wj[j] = weights[r * k + j0 + j];
+          wj[j] = weight_of(p >= 0, weights[r * k + j0 + j]);
           if (p >= 0) v[j].v = __builtin_nontemporal_load((const u32x4_t*)(y + (int64_t)p * d + c));
         }
       }
@@ -819,14 +820,16 @@ __global__ void __launch_bounds__(512) few_gate_up_kernel(FfnI8Args a, bf16_t* _
 template <int EPI>
 __global__ void __launch_bounds__(512) few_down_kernel(FfnI8Args a, const bf16_t* __restrict__ h) {
   extern __shared__ __attribute__((aligned(16))) int8_t q[];
-  __shared__ float y[64][16];
+  __shared__ float y[64][16], wj[64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 15;
   const int strips = a.d / 16, r = blockIdx.x / strips, c0 = blockIdx.x % strips * 16;
   int8_t* mine = q + wave * ((a.Fe + 63) / 64 * 64);
   for (int j = wave; j < a.k; j += 8) {
     const int id = a.ids[r * a.k + j];
+    const bool expert = id >= 0 && id < a.E;
+    const float w = a.weights[r * a.k + j];
     float v = 0.f;
-    if (id >= 0 && id < a.E) {
+    if (expert) {
       FewRow<64, kFewMaxFe / 512> hr;
       hr.load(h + ((int64_t)r * a.k + j) * a.Fe, a.Fe, lane);
       const int64_t col = (int64_t)id * a.d + c0 + fr;
@@ -842,11 +845,12 @@ __global__ void __launch_bounds__(512) few_down_kernel(FfnI8Args a, const bf16_t
       v = bf16_to_f32(f32_to_bf16((float)s.sum(mine, 0, a.Fe) * scale * s_down));
     }
     if (lane < 16) y[j][lane] = v;
+    if (lane == 0) wj[j] = weight_of(expert, w);
   }
   __syncthreads();
   if (tid < 16) {
     float s = 0.f;
-    for (int j = 0; j < a.k; ++j) s = fmaf(a.weights[r * a.k + j], y[j][tid], s);
+    for (int j = 0; j < a.k; ++j) s = fmaf(wj[j], y[j][tid], s);
     epi_store<EPI>(a.out, a.d, INT32_MAX, r, c0 + tid, s);
   }
 }
