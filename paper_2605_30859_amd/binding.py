@@ -144,16 +144,37 @@ def _ptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
+def _torch_calls():
+    """(current device, its current stream's handle).  torch.cuda.current_stream() makes an object in 2.6 us, a third
+    of a small call."""
+    global _device, _current_stream
+    import torch
+    _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+        lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
+_device = _current_stream = None
+
+
 def _stream(stream):
-    """The stream's handle; None: torch's current stream of the current device.  (A
-    torch.cuda.current_stream() object costs 2.6 us, a third of a small call.)"""
+    """The stream's handle; None: torch's current stream of the current device."""
     if stream is not None:
         return stream.cuda_stream
+    if _device is None:
+        _torch_calls()
     import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is None:
-        return torch.cuda.current_stream().cuda_stream
-    return raw(torch.cuda.current_device())
+    return _current_stream(torch.cuda.current_device())
+
+
+def _stream_of(x, stream):
+    """The stream's handle for a call on x, which has to be on the current device."""
+    if _device is None:
+        _torch_calls()
+    dev = x.get_device()
+    if dev < 0 or dev != _device():
+        raise ValueError(f"operands on {x.device}, which is not the current GPU")
+    return _current_stream(dev) if stream is None else stream.cuda_stream
 
 
 def _check(status, ctx=None):
@@ -266,24 +287,46 @@ def darts_gemm(a, w, c, M, N, K, dtype, epilogue, workspace=None, stream=None):
 def _rows_of(x):
     """(rows, columns, elements from one row to the next) of a matrix whose rows are contiguous."""
     rows, cols = x.shape
+    if x.is_contiguous():
+        return rows, cols, cols
     if cols > 1 and x.stride(1) != 1:
         raise ValueError("the elements of a row must be adjacent")
     return rows, cols, x.stride(0) if rows > 1 else cols
+
+
+def _dense(t, size, count):
+    """The address of t: a dense tensor of at least count elements of size bytes.  (As many bytes leave no room for
+    another type.)"""
+    n = t.nbytes
+    if t.is_contiguous() and (n == size * count or n > size * count and t.element_size() == size):
+        return t.data_ptr()
+    raise ValueError(f"wanted a dense tensor of at least {count} elements of {size} bytes, got {tuple(t.shape)} "
+                     f"{t.dtype} with strides {t.stride()}")
+
+
+def _rows_at(x, dtype):
+    """The address of rows whose elements have the size that dtype gives them."""
+    if x.element_size() != (2 if dtype == DARTS_BF16 else 4):
+        raise ValueError(f"rows of {x.dtype}, which is not the type {dtype}")
+    return x.data_ptr()
 
 
 def darts_moe_route(logits, dtype, ids, weights, score=SCORE_SOFTMAX, bias=None, n_groups=1, top_groups=1,
                     group_best=1, renorm=True, factor=1.0, stream=None):
     """logits [n_rows, n_experts] (rows may be strided); ids int32 and weights float32 [n_rows, top_k], written."""
     n_rows, n_experts, ld = _rows_of(logits)
-    _check(load_library().darts_moe_route(_ptr(logits), ld, n_rows, n_experts, dtype, score, _ptr(bias), n_groups,
-                                          top_groups, group_best, ids.shape[1], int(renorm), factor, _ptr(ids),
-                                          _ptr(weights), _stream(stream)))
+    top_k = ids.shape[1]
+    _check((_lib or load_library()).darts_moe_route(
+        _rows_at(logits, dtype), ld, n_rows, n_experts, dtype, score, None if bias is None else _dense(bias, 4, n_experts),
+        n_groups, top_groups, group_best, top_k, int(renorm), factor, _dense(ids, 4, n_rows * top_k),
+        _dense(weights, 4, n_rows * top_k), _stream_of(logits, stream)))
 
 
 def darts_quantize_rows(x, dtype, q, scale, stream=None):
     """x [rows, cols] (rows may be strided); q int8 [rows, cols] and scale float32 [rows], written."""
     rows, cols, ldx = _rows_of(x)
-    _check(load_library().darts_quantize_rows(_ptr(x), ldx, rows, cols, dtype, _ptr(q), _ptr(scale), _stream(stream)))
+    _check((_lib or load_library()).darts_quantize_rows(
+        _rows_at(x, dtype), ldx, rows, cols, dtype, _dense(q, 1, rows * cols), _dense(scale, 4, rows), _stream_of(x, stream)))
 
 
 def darts_gemm_i8_workspace_bytes(M, N, K):
@@ -291,9 +334,12 @@ def darts_gemm_i8_workspace_bytes(M, N, K):
 
 
 def darts_gemm_i8(a, a_scale, w, w_scale, c, M, N, K, epilogue, workspace=None, stream=None):
-    wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(load_library().darts_gemm_i8(_ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(c), M, N, K, epilogue,
-                                        _ptr(workspace) if wb else None, wb, _stream(stream)))
+    """a int8 [M, K], w int8 [N, K], scales float32 [M] and [N]; c float32 (epilogues 0 and 2) or bf16 (1 and 3)."""
+    wb = 0 if workspace is None else workspace.nbytes
+    _check((_lib or load_library()).darts_gemm_i8(
+        _dense(a, 1, M * K), _dense(a_scale, 4, M), _dense(w, 1, N * K), _dense(w_scale, 4, N),
+        _dense(c, 2 if epilogue & 1 else 4, M * N // 2 if epilogue == 3 else M * N), M, N, K, epilogue,
+        _dense(workspace, workspace.element_size(), 0) if wb else None, wb, _stream_of(a, stream)))
 
 
 def darts_moe_ffn_i8_workspace_bytes(n_rows, d_model, n_experts, top_k, expert_ffn):
@@ -304,10 +350,13 @@ def darts_moe_ffn_i8(x, ids, weights, n_experts, expert_ffn, w_gu, s_gu, w_down,
                      stream=None):
     """x [n_rows, d_model] bf16; ids, weights [n_rows, top_k]; out bf16 (epilogue 1) or float32, added to (2)."""
     n_rows, d_model = x.shape
-    _check(load_library().darts_moe_ffn_i8(_ptr(x), _ptr(ids), _ptr(weights), n_rows, d_model, n_experts,
-                                           ids.shape[1], expert_ffn, _ptr(w_gu), _ptr(s_gu), _ptr(w_down),
-                                           _ptr(s_down), _ptr(out), epilogue, _ptr(workspace),
-                                           workspace.numel() * workspace.element_size(), _stream(stream)))
+    top_k = ids.shape[1]
+    pairs, hidden, elements = n_rows * top_k, n_experts * expert_ffn, n_rows * d_model
+    _check((_lib or load_library()).darts_moe_ffn_i8(
+        _dense(x, 2, elements), _dense(ids, 4, pairs), _dense(weights, 4, pairs), n_rows, d_model, n_experts, top_k,
+        expert_ffn, _dense(w_gu, 1, 2 * hidden * d_model), _dense(s_gu, 4, 2 * hidden), _dense(w_down, 1, hidden * d_model),
+        _dense(s_down, 4, n_experts * d_model), _dense(out, 4 if epilogue == 2 else 2, elements), epilogue,
+        _dense(workspace, workspace.element_size(), 0), workspace.nbytes, _stream_of(x, stream)))
 
 
 def darts_debug_gemm_plan(M, N, K, epilogue):
