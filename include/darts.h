@@ -641,7 +641,8 @@ int darts_quantize_rows(const void* d_x, int64_t ldx, int32_t rows, int32_t cols
  *   d_a [M][K], d_w [N][K] codes, 16-byte aligned as d_c is; K and N multiples of
  *   16 (N of 32 for SwiGLU), K <= 131072 (so that the sum fits), and fewer than 2^24
  *   tiles of 64 x 64 results.  d_workspace must hold
- *   darts_gemm_i8_workspace_bytes(M, N, K) bytes, 16-byte aligned.         */
+ *   darts_gemm_i8_workspace_bytes(M, N, K) bytes, 16-byte aligned, of its own for
+ *   calls that overlap in time, captured graphs too.                       */
 size_t darts_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K);
 int darts_gemm_i8(const int8_t* d_a, const float* d_a_scale, const int8_t* d_w, const float* d_w_scale,
                   void* d_c, int32_t M, int32_t N, int32_t K, int32_t epilogue, void* d_workspace,
@@ -671,6 +672,20 @@ int darts_moe_ffn_i8(const void* d_x, const int32_t* d_ids, const float* d_weigh
                      int32_t d_model, int32_t n_experts, int32_t top_k, int32_t expert_ffn,
                      const int8_t* d_w_gu, const float* d_s_gu, const int8_t* d_w_down, const float* d_s_down,
                      void* d_out, int32_t epilogue, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* The kernels that run an 8-bit call (host only), for tests that have to reach each.
+ * darts_debug_gemm_i8_plan: out[0..4] = 0 for weights straight into registers (a few
+ * rows), 1 for the LDS ring, 2 for the alternating groups; rows and channels of a
+ * tile; K splits (of the first: wavefronts that share 16 channels); 1 if the rows of
+ * d_a are copied into padded ones first.
+ * darts_debug_moe_ffn_i8_plan: out[0..5] = 0 for weights per (row, slot) pair (the
+ * rest is 0), 1 for routing lists in the first launch, 2 in launches of their own;
+ * rows of a tile; its channels in the gate/up and in the down product; 1 if that
+ * product's K is no multiple of 256, for both.
+ * DARTS_EINVAL for no rows and for sizes that the calls refuse.                 */
+int darts_debug_gemm_i8_plan(int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t* out);
+int darts_debug_moe_ffn_i8_plan(int32_t n_rows, int32_t d_model, int32_t n_experts, int32_t top_k, int32_t expert_ffn,
+                                int32_t* out);
 
 #ifdef __cplusplus
 }

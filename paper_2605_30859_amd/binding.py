@@ -115,6 +115,8 @@ _SIGS = {
     "darts_moe_ffn_i8_workspace_bytes": (C.c_size_t, [C.c_int32] * 5),
     "darts_moe_ffn_i8": (C.c_int, [_P, _P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, _P,
                                    _P, _P, _P, C.c_int32, _P, C.c_size_t, _P]),
+    "darts_debug_gemm_i8_plan": (C.c_int, [C.c_int32] * 4 + [_P]),
+    "darts_debug_moe_ffn_i8_plan": (C.c_int, [C.c_int32] * 5 + [_P]),
     "darts_select_groups": (C.c_int, [_P, _P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                       C.c_int32, C.c_int32, _P, _P, _P, _P, _P, _P, _P, _P]),
 }
@@ -364,6 +366,21 @@ def darts_debug_gemm_plan(M, N, K, epilogue):
     darts_gemm call."""
     out = (C.c_int32 * 6)()
     _check(load_library().darts_debug_gemm_plan(M, N, K, epilogue, out))
+    return tuple(out)
+
+
+def darts_debug_gemm_i8_plan(M, N, K, epilogue):
+    """(kernel, tile rows, tile channels, K splits, padded rows) of a darts_gemm_i8 call."""
+    out = (C.c_int32 * 5)()
+    _check(load_library().darts_debug_gemm_i8_plan(M, N, K, epilogue, out))
+    return tuple(out)
+
+
+def darts_debug_moe_ffn_i8_plan(n_rows, d_model, n_experts, top_k, expert_ffn):
+    """(lists, tile rows, channels of gate/up tiles, of down tiles, short K of gate/up, of down) of a darts_moe_ffn_i8
+    call."""
+    out = (C.c_int32 * 6)()
+    _check(load_library().darts_debug_moe_ffn_i8_plan(n_rows, d_model, n_experts, top_k, expert_ffn, out))
     return tuple(out)
 
 

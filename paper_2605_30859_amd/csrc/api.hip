@@ -1417,12 +1417,16 @@ size_t darts_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K) {
   return gemm_i8_workspace_bytes(M, N, K);
 }
 
+static bool gemm_i8_sizes(int32_t M, int32_t N, int32_t K, int32_t epilogue) {
+  if (M < 0 || N < 1 || K < 1 || N % 16 || K % 16 || K > kI8MaxK) return false;
+  if (epilogue < 0 || epilogue > 3 || (epilogue == 3 && N % 32)) return false;
+  return ((int64_t)M + 63) / 64 * (((int64_t)N + 63) / 64) < (1 << 24);   // tiles of a launch
+}
+
 int darts_gemm_i8(const int8_t* d_a, const float* d_a_scale, const int8_t* d_w, const float* d_w_scale,
                   void* d_c, int32_t M, int32_t N, int32_t K, int32_t epilogue, void* d_workspace,
                   size_t workspace_bytes, void* stream) {
-  if (M < 0 || N < 1 || K < 1 || N % 16 || K % 16 || K > kI8MaxK) return DARTS_EINVAL;
-  if (epilogue < 0 || epilogue > 3 || (epilogue == 3 && N % 32)) return DARTS_EINVAL;
-  if (((int64_t)M + 63) / 64 * (((int64_t)N + 63) / 64) >= (1 << 24)) return DARTS_EINVAL;   // too many tiles for a launch
+  if (!gemm_i8_sizes(M, N, K, epilogue)) return DARTS_EINVAL;
   if (M == 0) return DARTS_OK;
   if (!d_a || !d_a_scale || !d_w || !d_w_scale || !d_c) return DARTS_EINVAL;
   if (!aligned16(d_a) || !aligned16(d_w) || !aligned16(d_c) || !aligned16(d_workspace)) return DARTS_EINVAL;
@@ -1431,6 +1435,11 @@ int darts_gemm_i8(const int8_t* d_a, const float* d_a_scale, const int8_t* d_w, 
   hipError_t e = launch_gemm_i8(d_a, d_a_scale, d_w, d_w_scale, d_c, M, N, K, epilogue, d_workspace, workspace_bytes,
                                 (hipStream_t)stream);
   return e == hipSuccess ? DARTS_OK : DARTS_EHIP;
+}
+
+int darts_debug_gemm_i8_plan(int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t* out) {
+  if (M < 1 || !gemm_i8_sizes(M, N, K, epilogue) || !out) return DARTS_EINVAL;
+  return gemm_i8_plan_info(M, N, K, epilogue, out) ? DARTS_OK : DARTS_EINVAL;
 }
 
 static bool ffn_i8_sizes(int32_t n_rows, int32_t d, int32_t E, int32_t k, int32_t Fe) {
@@ -1443,6 +1452,13 @@ size_t darts_moe_ffn_i8_workspace_bytes(int32_t n_rows, int32_t d_model, int32_t
                                         int32_t expert_ffn) {
   if (n_rows < 1 || !ffn_i8_sizes(n_rows, d_model, n_experts, top_k, expert_ffn)) return 0;
   return moe_ffn_i8_workspace_bytes(n_rows, d_model, n_experts, top_k, expert_ffn);
+}
+
+int darts_debug_moe_ffn_i8_plan(int32_t n_rows, int32_t d_model, int32_t n_experts, int32_t top_k, int32_t expert_ffn,
+                                int32_t* out) {
+  if (n_rows < 1 || !ffn_i8_sizes(n_rows, d_model, n_experts, top_k, expert_ffn) || !out) return DARTS_EINVAL;
+  moe_ffn_i8_plan_info(n_rows, d_model, n_experts, top_k, expert_ffn, out);
+  return DARTS_OK;
 }
 
 int darts_moe_ffn_i8(const void* d_x, const int32_t* d_ids, const float* d_weights, int32_t n_rows,

@@ -434,6 +434,21 @@ size_t gemm_i8_workspace_bytes(int M, int N, int K) {
   return plan_i8(p, M, N, K) ? plan_ws_bytes(p, M, N) : 0;
 }
 
+bool gemm_i8_plan_info(int M, int N, int K, int epi, int32_t* out) {
+  I8Plan p;
+  if (!plan_i8(p, M, N, K)) return false;
+  if (p.kind < 0) {
+    const int wk = epi == EPI_SWIGLU ? 4 : p.S;        // as skinny_i8 has them
+    const int32_t v[5] = {0, M <= 16 ? 16 : 32, 8 / wk * 16, wk, 0};
+    std::copy(v, v + 5, out);
+  } else {
+    const I8Tiles& t = kI8Tiles[p.kind];
+    const int32_t v[5] = {t.alt ? 2 : 1, t.bm, t.bn, p.S, p.pad};
+    std::copy(v, v + 5, out);
+  }
+  return true;
+}
+
 // Rows of K codes to rows of ldo, with zeros behind them; 16 bytes per thread.
 __global__ void __launch_bounds__(256) pad_rows_kernel(const int8_t* __restrict__ a, int64_t rows, int K, int ldo,
                                                        int8_t* __restrict__ out) {
@@ -630,6 +645,13 @@ static bool grouped_i8_wide(int64_t pairs, int E, int N) {
   return pairs >= (int64_t)24 * E && std::min<int64_t>(pairs, E) * ((N + 255) / 256) >= 2 * kI8Cus;
 }
 
+// Channels of a tile of so many rows.
+static int grouped_i8_cols(int rows, int64_t pairs, int E, int N) {
+  return rows == 256 || grouped_i8_wide(pairs, E, N) ? 256 : 128;
+}
+// Whether the weights end inside the last pair of K tiles.
+static bool grouped_i8_short(int K) { return K % 256 != 0; }
+
 template <int BM, int BN, int BPC, int EPI, int WAUX, bool TAIL>
 static hipError_t grouped_alt(const I8Call& c, const I8Groups& g, hipStream_t st) {
   constexpr int lds = 2 * (BM + BN) * 64 * 2 + kAltScaleBytes;
@@ -643,15 +665,15 @@ static hipError_t grouped_alt(const I8Call& c, const I8Groups& g, hipStream_t st
 }
 template <int BM, int BN, int BPC, int EPI, int WAUX>
 static hipError_t grouped_tail(const I8Call& c, const I8Groups& g, hipStream_t st) {
-  return c.K % 256 ? grouped_alt<BM, BN, BPC, EPI, WAUX, true>(c, g, st)
+  return grouped_i8_short(c.K) ? grouped_alt<BM, BN, BPC, EPI, WAUX, true>(c, g, st)
                    : grouped_alt<BM, BN, BPC, EPI, WAUX, false>(c, g, st);
 }
 // c.M: the routed rows.
 template <int EPI>
 static hipError_t grouped_i8(int rows, int E, const I8Call& c, const I8Groups& g, hipStream_t st) {
   if (rows == 256) return grouped_tail<256, 256, 1, EPI, 0>(c, g, st);
-  return grouped_i8_wide(c.M, E, c.N) ? grouped_tail<128, 256, 1, EPI, kNtLoad>(c, g, st)
-                                      : grouped_tail<128, 128, 2, EPI, kNtLoad>(c, g, st);
+  return grouped_i8_cols(rows, c.M, E, c.N) == 256 ? grouped_tail<128, 256, 1, EPI, kNtLoad>(c, g, st)
+                                                   : grouped_tail<128, 128, 2, EPI, kNtLoad>(c, g, st);
 }
 
 // ------------------------------------------------------------ routed experts
@@ -915,10 +937,22 @@ size_t moe_ffn_i8_workspace_bytes(int64_t rows, int d, int E, int k, int Fe) {
 // (2048, 768), 8 each: 1 row 13 / 32, 4 rows 30 / 46, 10 rows 64 / 68; 64 experts
 // (1024, 1408), 6 each: 4 rows 24 / 39, 7 rows 35 / 49; 60 experts (1456, 720), 4
 // each: 10 rows 30 / 48; 16 experts (1024, 512), 4 each: 1 row 8 / 25, 15 rows 18 / 27.
-static bool few_rows(const FfnI8Args& a) {
-  const int64_t pairs = (int64_t)a.n_rows * a.k;
-  return (3 * pairs <= 2 * a.E || (pairs <= 72 && 3 * pairs * a.d * a.Fe <= 250000000)) && a.d <= kFewMaxD &&
-         a.Fe <= kFewMaxFe;
+static bool few_rows(int64_t pairs, int d, int E, int Fe) {
+  return (3 * pairs <= 2 * E || (pairs <= 72 && 3 * pairs * d * Fe <= 250000000)) && d <= kFewMaxD && Fe <= kFewMaxFe;
+}
+
+void moe_ffn_i8_plan_info(int n_rows, int d, int E, int k, int Fe, int32_t* out) {
+  const int pairs = n_rows * k, rows = grouped_i8_rows(pairs, E);
+  int32_t v[6] = {0, 0, 0, 0, 0, 0};
+  if (!few_rows(pairs, d, E, Fe)) {
+    v[0] = pairs <= kMoeOneBlockPairs ? 1 : 2;
+    v[1] = rows;
+    v[2] = grouped_i8_cols(rows, pairs, E, 2 * Fe);
+    v[3] = grouped_i8_cols(rows, pairs, E, d);
+    v[4] = grouped_i8_short(d);
+    v[5] = grouped_i8_short(Fe);
+  }
+  std::copy(v, v + 6, out);
 }
 
 hipError_t launch_moe_ffn_i8(const FfnI8Args& a, hipStream_t st) {
@@ -926,7 +960,7 @@ hipError_t launch_moe_ffn_i8(const FfnI8Args& a, hipStream_t st) {
   FfnWork f;
   if (ffn_layout(a.n_rows, a.d, a.E, a.k, a.Fe, (char*)a.ws, &f) > a.ws_bytes) return hipErrorInvalidValue;
   const int n_pairs = a.n_rows * a.k;
-  if (few_rows(a)) {
+  if (few_rows(n_pairs, a.d, a.E, a.Fe)) {
     hipLaunchKernelGGL(few_gate_up_kernel, dim3(n_pairs * (a.Fe / 16)), dim3(512), (a.d + 63) / 64 * 64, st, a, f.h);
     const dim3 grid(a.n_rows * (a.d / 16));
     const int lds = 8 * ((a.Fe + 63) / 64 * 64);

@@ -300,6 +300,10 @@ hipError_t launch_quantize_rows(const void* x, int64_t rows, int cols, int64_t l
 size_t gemm_i8_workspace_bytes(int M, int N, int K);
 hipError_t launch_gemm_i8(const int8_t* a, const float* a_scale, const int8_t* w, const float* w_scale, void* c, int M,
                           int N, int K, int epi, void* ws, size_t ws_bytes, hipStream_t st);
+// kernel, tile rows and channels, splits, padded copy (5 values); false without a plan
+bool gemm_i8_plan_info(int M, int N, int K, int epi, int32_t* out);
+// lists, tile rows, tile channels and short last K tiles of gate/up and down (6 values)
+void moe_ffn_i8_plan_info(int n_rows, int d, int E, int k, int Fe, int32_t* out);
 size_t moe_ffn_i8_workspace_bytes(int64_t rows, int d, int E, int k, int Fe);
 struct FfnI8Args {
   const void* x; const int32_t* ids; const float* weights;   // [n_rows][d] bf16, [n_rows][k]
