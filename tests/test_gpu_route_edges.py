@@ -1,5 +1,6 @@
-"""The router (darts_moe_route) where finite biases are as large as float32 holds:
-ids equal to the float64 oracle's, weights within one float32 rounding."""
+"""The router (darts_moe_route) where finite biases are as large as float32 holds, and at
+sizes that reach each of its kernels: ids equal to the float64 oracle's, weights within
+one float32 rounding."""
 import numpy as np
 import pytest
 
@@ -20,7 +21,7 @@ def _check(logits, k, score, bias, **kw):
     B.darts_moe_route(logits, B.DARTS_F32, ids, w, score=B.SCORE_SIGMOID if score == "sigmoid" else B.SCORE_SOFTMAX,
                       bias=bias, **kw)
     ids, w = ids.cpu().numpy(), w.cpu().numpy()
-    eid, ew = route(logits.cpu().numpy(), k, score=score, bias=bias.cpu().numpy(), **kw)
+    eid, ew = route(logits.cpu().numpy(), k, score=score, bias=None if bias is None else bias.cpu().numpy(), **kw)
     assert (ids == eid).all(), np.argwhere(ids != eid)[:5]
     assert (np.abs(w - ew) <= np.abs(ew) * (2.0 ** -24 * (1 + 1e-6)) + 2.0 ** -149).all()
 
@@ -58,3 +59,31 @@ def test_groups_of_biases_near_the_ends_of_float32(name, E, k, best):
     for score in ("softmax", "sigmoid"):
         for top in (1, 2, 3, 5):
             _check(_logits(37, E), k, score, bias, n_groups=8, top_groups=top, group_best=best)
+
+
+# experts, experts of a row, groups: 16, 32 and 64 lanes a row with 4, 8 and 16 experts
+# each, in the order of logits or scores and by groups; groups of other sizes and 64
+# experts a row, which go by the definition alone
+SIZES = [(60, 5, 1), (64, 15, 8), (37, 9, 1), (128, 15, 8), (100, 7, 1), (120, 15, 1), (64, 20, 4), (256, 31, 8), (200, 9, 1),
+         (129, 16, 3), (512, 40, 8), (300, 33, 1), (128, 63, 16), (1024, 63, 8), (1000, 10, 1), (1024, 63, 64), (777, 31, 7),
+         (48, 6, 4), (96, 8, 4), (160, 6, 8), (320, 12, 10), (600, 8, 6), (64, 64, 1), (200, 64, 1), (512, 64, 8), (1000, 64, 5)]
+
+
+@pytest.mark.parametrize("E,k,groups", SIZES)
+@pytest.mark.parametrize("first", [0, 1])
+def test_every_kernel(E, k, groups, first):
+    """Rows that begin at addresses for wide loads, and rows that do not."""
+    print(f"route {E} {k} {groups} from element {first}", flush=True)
+    rows = 43
+    g = torch.Generator(device=DEV).manual_seed(E + k)
+    ld = E + (-E) % 8 + first
+    flat = torch.empty(rows * ld + 8, device=DEV).normal_(0.0, 1.5, generator=g)
+    bias = torch.empty(E, device=DEV).normal_(0.0, 0.1, generator=g)
+    l = torch.as_strided(flat, (rows, E), (ld, 1), first)
+    l[3], l[4, : E // 2], l[5, 1:] = -INF, -INF, -INF
+    for score in ("softmax", "sigmoid"):
+        for b in (bias, torch.zeros_like(bias)):
+            for best in (1, 2) if groups > 1 else (1,):
+                kw = dict(n_groups=groups, top_groups=(groups + 1) // 2, group_best=best)
+                _check(l, k, score, b, **kw)
+        _check(l, k, score, None)
