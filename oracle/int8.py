@@ -3,9 +3,9 @@ plain statement of what the library's 8-bit entries compute.
 
 Codes are defined by float32 arithmetic (two divisions, a product, a rounding to
 the nearest integer with halves to even) and reproduced as such; everything
-behind them is float64, with the roundings to bf16 that the definition has
-(hidden activations, and the results that are stored in bf16 by the caller's
-choice are left unrounded).
+behind them is float64, with the roundings to bf16 that the definition has:
+hidden activations, and each expert's result before the weighted sum.  Results
+that are stored in bf16 by the caller's choice are left unrounded.
 
 Pins (tests/test_oracle_int8.py): closed forms and hand examples of the codes,
 the error of a code and its scale (at most half a step), integer products in
@@ -58,9 +58,9 @@ def product(a, a_scale, w, w_scale):
 
 
 def expert(x, w_gu, s_gu, w_down, s_down):
-    """One expert's rows: x float32 (bf16 values) -> float64."""
+    """One expert's rows: x float32 (bf16 values) -> float64 (bf16 values)."""
     h = round_bf16(swiglu(product(*quantize_rows(x), w_gu, s_gu)))
-    return product(*quantize_rows(h), w_down, s_down)
+    return round_bf16(product(*quantize_rows(h), w_down, s_down)).astype(np.float64)
 
 
 def moe_ffn(x, ids, weights, w_gu, s_gu, w_down, s_down):
