@@ -398,14 +398,18 @@ static double i8_estimate(const I8Plan& p, int M, int N, int K) {
 // Skinny: a few rows; up to 16 of them while the weights are small (16 rows: 4096 x
 // 4096 6.9 us against 9.1 in tiles, 6144 x 4096 10.5 against 10.9, 4096 x 12288 15.6
 // against 15.1, 24576 x 4096 30 against 23), up to 32 while K is short, too (32 rows:
-// 8192 x 1024 6.0 against 6.6, 2048 x 4096 9.2 against 8.7).  Eight wavefronts per
-// strip, or four of twice the range where the strips alone give enough of them (one
-// row: 6144 x 4096 7.7 us with four, 8.2 with eight; 2048 x 4096 6.9 and 5.1; 12288 x
-// 8192 23 and 20).
+// 8192 x 1024 6.0 against 6.6, 2048 x 4096 9.2 against 8.7).
+// Eight wavefronts per strip, a block; or four of twice the range and two strips a
+// block, where that makes one round of blocks over the CUs of two, or K is too short to
+// tell.  One row, four and eight, us: 4096 x 4096 7.5 / 6.2, 4608 x 4096 7.7 / 8.4, 6144 x
+// 4096 8.1 / 8.7, 8192 x 4096 9.2 / 9.1, 12288 x 4096 14.5 / 12.0, 24576 x 4096 24.3 /
+// 23.0; 6144 x 8192 13.7 / 15.0, 12288 x 8192 27.8 / 25.4; 4608 x 2048 5.2 / 5.3, 10240 x
+// 2048 8.5 / 7.0; 6144 x 512 3.2 / 3.7, 12288 x 512 3.9 / 4.4.  16 rows alike.
 static bool skinny_i8_plan(I8Plan& p, int M, int N, int K) {
   const int64_t w = (int64_t)N * K;
   if (M > 4 && !(M <= 16 && w <= 26000000) && !(M <= 32 && w <= 8400000 && K <= 2048)) return false;
-  return set_i8_plan(p, -1, N >= 16 * 384 && K <= 4096 ? 4 : 8, M, N, K);
+  const int strips = (N + 15) / 16;
+  return set_i8_plan(p, -1, strips > kI8Cus && (strips <= 2 * kI8Cus || K <= 512) ? 4 : 8, M, N, K);
 }
 
 // False if the results are too many for any (2^36 elements).

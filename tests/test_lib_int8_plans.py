@@ -81,3 +81,11 @@ def test_plans_refuse_what_the_calls_refuse():
         assert lib.darts_debug_moe_ffn_i8_plan(R, d, E, k, F, out) == B.DARTS_EINVAL
     assert lib.darts_debug_gemm_i8_plan(4, 64, 64, 0, None) == B.DARTS_EINVAL
     assert lib.darts_debug_moe_ffn_i8_plan(4, 64, 8, 2, 32, None) == B.DARTS_EINVAL
+
+
+@pytest.mark.parametrize("N,K,wavefronts", [(2048, 4096, 8), (4096, 4096, 8), (4096, 512, 8), (4112, 4096, 4), (5120, 2048, 4),
+                                            (5120, 8192, 4), (6144, 4096, 4), (8192, 4096, 4), (8208, 4096, 8),
+                                            (12288, 4096, 8), (24576, 4096, 8), (12288, 512, 4), (24576, 512, 4)])
+def test_wavefronts_of_a_strip_go_by_rounds_of_blocks(N, K, wavefronts):
+    """Four where two strips a block make one round over the CUs of two, or K is short."""
+    assert B.darts_debug_gemm_i8_plan(1, N, K, 0)[3] == wavefronts
