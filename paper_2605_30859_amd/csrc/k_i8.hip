@@ -682,9 +682,15 @@ static hipError_t grouped_i8(int rows, int E, const I8Call& c, const I8Groups& g
 
 // ------------------------------------------------------------ routed experts
 // out[r] = sum_j w[r][j] * y[pos(r, j)] in slot order, fp32 sums, 8 columns per
-// thread; y is read once, non-temporal (a layer of 8000 rows 482 us, 590 with plain
-// loads; 32768 rows 1657 and 1785).  A place without an expert adds nothing, whatever
-// its weight, but NaN for the weight NaN of a row that the router could not read.
+// thread; y is read once, non-temporal (a layer of 8000 rows 512 us, 516 with plain
+// loads; 32768 rows 1750 and 1787).  y is bf16, as in the decoder's bf16 experts: half
+// the bytes that the down product and this sum exchange.  Measured with a float32 y in
+// its place: one row 12.0 us (bf16 12.1), 61 rows 109 (106), 976 rows 179 (167), 32768
+// rows 2250 (1730); the error of a bf16 result against 64 bits, relative in the 2-norm,
+// 0.0017 (0.0023).  The two launches of a few rows round y, too, so that a row's result
+// does not hang on how many come with it.
+// A place without an expert adds nothing, whatever its weight, but NaN for the weight
+// NaN of a row that the router could not read.
 __device__ __forceinline__ float weight_of(bool expert, float w) { return expert || w != w ? w : 0.f; }
 template <int EPI>
 __global__ void __launch_bounds__(256) combine_i8_kernel(const bf16_t* __restrict__ y, int d, int k,
